@@ -458,6 +458,113 @@ int elitekv_slrd_decode_step(const elitekv_dims* dims, int32_t d_ck, const void*
                              size_t ws_bytes, int32_t n_splits, void* hip_stream);
 
 /* ---------------------------------------------------------------------------------------------
+ * A cache in pages.  A page is page_rows rows of both planes (a power of two from 16 to 2^20), page p the plane rows
+ * [p * page_rows, (p + 1) * page_rows); row b of block_table [B, table_cols] int32 lists request b's pages: cached token j of
+ * request b lies in plane row
+ *     block_table[b, j / page_rows] * page_rows + j % page_rows.
+ * What a token's row holds is as everywhere (Sections 3.1 and 3.2, what enters the cache): elitekv_append and elitekv_slrd_append
+ * write such a cache as it is, with the slots that elitekv_page_plan answers.  Both planes share the table.
+ * ------------------------------------------------------------------------------------------- */
+
+/*
+ * Pages by request lengths, and where every new token goes.  Request b has cached_len[b] tokens in its cache and is about to append
+ * new_len[b] more; after the call it holds
+ *     held_out[b] = min(ceil((cached_len[b] + new_len[b]) / page_rows), table_cols)   pages,
+ * the first entries of its row of the table: what it lacked has been taken from the free pages, what it held beyond that has gone
+ * back to them (a request that has ended, or whose drafted tokens were rejected, says so by its lengths).  Entries that stay are not
+ * touched.  For every token t < T of request b:
+ *     pos[b, t] = cached_len[b] + t, slot[b, t] = its plane row, kv_len[b, t] = pos[b, t] + 1,
+ * the arguments of elitekv_append (slot), elitekv_paged_attn and _multiquery_attn (kv_len); for t >= new_len[b] 0, -1 and 0: no
+ * token is stored and nothing attended.
+ * The free pages are a ring: free_pages [n_pages] int32 holds, at the places free_span[0] .. free_span[1] - 1 modulo n_pages, the
+ * pages that nobody holds.  Pages are taken from the front, in the order of the requests and of their tables, and go back to the end
+ * in the same order; free_span_out has the two counts after the call.  At the start of a server: free_pages = 0 .. n_pages - 1,
+ * free_span = {0, n_pages}, held = 0.  Pages that go back in a call are not handed out in the same call.  Where the free pages do not
+ * suffice, requests are served in their order and the rest keeps what it has: held_out[b] is smaller than the length asks for, and
+ * the tokens without a page get slot -1 and kv_len 0.
+ *   cached_len, new_len, held, held_out  [B] int32 (held_out may be held); negative lengths count as 0, new_len above T as T
+ *   free_span, free_span_out             [2] int64 (may be the same)
+ *   pos, kv_len [B, T] int32, slot [B, T] int64
+ *   ws         elitekv_page_plan_workspace_bytes(B, T) bytes
+ * A page that two requests hold goes back twice; the caller keeps count of shared ones.  Nothing outside the arrays is touched
+ * whatever the arrays hold.  Whole numbers throughout, the same result however the call is executed.  B == 0 is a successful no-op.
+ * Errors: EINVAL (page_rows, n_pages < 1, table_cols < 1, T < 1), ENULL, EALIGN (ws), EWORKSPACE, EUNSUPPORTED (B > 65535,
+ * T > 65536), EHIP.
+ */
+size_t elitekv_page_plan_workspace_bytes(int64_t B, int64_t T);
+int elitekv_page_plan(const int32_t* cached_len, const int32_t* new_len, int64_t B, int64_t T, int32_t page_rows, int32_t n_pages,
+                      int32_t* block_table, int32_t table_cols, const int32_t* held, int32_t* held_out, int32_t* free_pages,
+                      const int64_t* free_span, int64_t* free_span_out, int32_t* pos, int64_t* slot, int32_t* kv_len, void* ws,
+                      size_t ws_bytes, void* hip_stream);
+
+/*
+ * elitekv_multiquery_attn (T = 1: elitekv_decode_attn) over a cache in pages, and with d_ck > 0 their slrd_ forms (W_uk = B^k_S,
+ * W_uv = B^v_S).  The arguments are theirs with the table in place of batch_stride_rows; kv_len is clamped to max_seq_len and to what
+ * the table has room for.  Of every request only pages that hold one of the first kv_len rows are read; a table entry outside
+ * [0, plane_rows / page_rows) counts as page 0.
+ * Workspace and errors as elitekv_multiquery_attn; EINVAL also for page_rows and table_cols < 1, ENULL without a table.
+ */
+size_t elitekv_paged_attn_workspace_bytes(const elitekv_dims* dims, int32_t d_ck, int64_t B, int64_t T, int64_t max_seq_len,
+                                          int32_t n_splits);
+int elitekv_paged_attn(const elitekv_dims* dims, int32_t d_ck, const void* q, const int32_t* q_pos, const int32_t* kv_len, int64_t B,
+                       int64_t T, int64_t max_seq_len, const int32_t* block_table, int32_t table_cols, int32_t page_rows,
+                       const void* W_uk, const void* W_uv, const int32_t* elite_idx, const void* ke_plane, const void* c_plane,
+                       int64_t plane_rows, void* out, void* ws, size_t ws_bytes, int32_t n_splits, void* hip_stream);
+
+/* ---------------------------------------------------------------------------------------------
+ * Drafted tokens as a tree.  The drafted tokens of a sequence are the nodes 0 .. n_nodes[b] - 1 of a tree (or of several), every
+ * node behind its parent; they lie in the cache behind the prefix_len[b] tokens of the sequence, node t in row prefix_len[b] + t, and
+ * have the position prefix_len[b] + depth.  A node attends to the prefix, to its ancestors and to itself (Section 2.1: K_t, V_t of
+ * the tokens up to step t, along the node's own path).  Up to ELITEKV_TREE_MAX_NODES nodes a sequence, T of them in the arrays.
+ * A step: elitekv_tree_plan, elitekv_append (its positions, slots by elitekv_page_plan or of the caller), elitekv_tree_attn, the
+ * caller's choice of a path, elitekv_tree_commit.
+ * ------------------------------------------------------------------------------------------- */
+#define ELITEKV_TREE_MAX_NODES 128
+
+/*
+ * Positions and masks of trees.  parent [B, T] int32: the parent of every node, an earlier node; any other value: a root.
+ *   pos  [B, T] int32                  prefix_len[b] + the node's depth (a root has 0); 0 for t >= n_nodes[b]
+ *   mask [B, T, ceil(T / 32)] uint32   bit j % 32 of word j / 32: node t sees node j; 0 for t >= n_nodes[b]
+ * Errors: EINVAL (T < 1, B < 0), EUNSUPPORTED (T > ELITEKV_TREE_MAX_NODES, B > 65535), ENULL, EHIP.
+ */
+int elitekv_tree_plan(const int32_t* parent, const int32_t* prefix_len, const int32_t* n_nodes, int64_t B, int64_t T, int32_t* pos,
+                      uint32_t* mask, void* hip_stream);
+
+/*
+ * Attention of the T nodes of every sequence: query (b, t) sees the rows [0, prefix_len[b]) of sequence b and, for every bit
+ * j < n_nodes[b] of mask[b, t], row prefix_len[b] + j.  Any mask is allowed, not only a tree's: several drafts beside each other,
+ * nodes that see later ones, a row without any bit; a query that sees nothing, and every t >= n_nodes[b], gets a zero output row.
+ * A row that a query does not see never reaches its result, whatever it holds.
+ *   q [B, T, n_h, d_h], q_pos [B * T], out [B, T, n_h, d_h]; prefix_len, n_nodes [B] int32; mask as elitekv_tree_plan answers it
+ *   max_seq_len          HOST upper bound of prefix_len + n_nodes: rows beyond it are not seen
+ *   block_table          a cache in pages (elitekv_paged_attn); NULL with page_rows = 0: rows back to back, sequence b from plane row
+ *                        b * batch_stride_rows on (which is not used otherwise)
+ *   d_ck                 0: joint latent; > 0: separated latents, W_uk = B^k_S, W_uv = B^v_S
+ * Other arguments, workspace rules and errors as elitekv_multiquery_attn; EUNSUPPORTED if T > ELITEKV_TREE_MAX_NODES.
+ */
+size_t elitekv_tree_attn_workspace_bytes(const elitekv_dims* dims, int32_t d_ck, int64_t B, int64_t T, int64_t max_seq_len,
+                                         int32_t n_splits);
+int elitekv_tree_attn(const elitekv_dims* dims, int32_t d_ck, const void* q, const int32_t* q_pos, const int32_t* prefix_len,
+                      const int32_t* n_nodes, const uint32_t* mask, int64_t B, int64_t T, int64_t max_seq_len,
+                      int64_t batch_stride_rows, const int32_t* block_table, int32_t table_cols, int32_t page_rows, const void* W_uk,
+                      const void* W_uv, const int32_t* elite_idx, const void* ke_plane, const void* c_plane, int64_t plane_rows,
+                      void* out, void* ws, size_t ws_bytes, int32_t n_splits, void* hip_stream);
+
+/*
+ * The accepted path becomes the sequence's next tokens: for k = 0 .. path_len[b] - 1, row prefix_len[b] + k of both planes takes
+ * what row prefix_len[b] + path[b, k] held before the call.  path [B, T] int32: the accepted nodes in the order of their depth, so
+ * path[b, k] >= k and a node's stored key, rotated to position prefix + depth, is that of the token in its new row (Section 3.1).
+ * An entry outside [k, T) leaves row k as it is, and so does a row that lies outside the planes, in a page that does not exist, or
+ * (rows back to back, batch_stride_rows > 0) beyond the sequence's batch_stride_rows rows.  The rows behind the path keep what they
+ * hold; the sequence has prefix_len[b] + path_len[b] tokens now.
+ * ke_plane may be NULL when r == 0.  Other arguments as elitekv_tree_attn.  Errors: EINVAL, ENULL, EALIGN (planes), EUNSUPPORTED
+ * (T > ELITEKV_TREE_MAX_NODES, B > 65535), EHIP.
+ */
+int elitekv_tree_commit(const elitekv_dims* dims, const int32_t* path, const int32_t* path_len, const int32_t* prefix_len, int64_t B,
+                        int64_t T, int64_t batch_stride_rows, const int32_t* block_table, int32_t table_cols, int32_t page_rows,
+                        void* ke_plane, void* c_plane, int64_t plane_rows, void* hip_stream);
+
+/* ---------------------------------------------------------------------------------------------
  * Measurement-only companions (not part of the method).
  * ------------------------------------------------------------------------------------------- */
 

@@ -328,6 +328,91 @@ def slrd_multiquery_attn(q, q_pos, ke, c_k, c_v, kv_len, B_k, B_v, elite_idx, he
 
 
 # ----------------------------------------------------------------------------------------------
+# A cache in pages and trees of drafted tokens.  Where a row lies and which rows a query sees are stated outright: rows are
+# gathered through the table one by one, and attention is the definition above over the rows that are seen, nothing else.
+# ----------------------------------------------------------------------------------------------
+def page_plan(cached, new, T: int, page: int, n_pages: int, table, held, free, span):
+    """Requests in their order take the pages they lack from the front of the ring and put what they hold beyond their need
+    at its end.  table [B, cols], held [B], free [n_pages], span (first, end).  Returns (table, held, free, span, pos, slot,
+    kv_len) as lists / arrays of integers; nothing is modified."""
+    table, free, held = np.array(table), np.array(free), [int(h) for h in held]
+    B, cols = table.shape
+    before, first, end = free.copy(), int(span[0]), int(span[1])
+    avail = min(max(end - first, 0), n_pages)
+    pos, slot, kv = np.zeros((B, T), np.int64), np.full((B, T), -1, np.int64), np.zeros((B, T), np.int64)
+    taken = 0
+    for b in range(B):
+        c, n = max(int(cached[b]), 0), min(max(int(new[b]), 0), T)
+        held[b] = min(max(held[b], 0), cols)
+        want = min(-(-(c + n) // page), cols)
+        while held[b] < want and taken < avail:
+            table[b, held[b]] = before[(first + taken) % n_pages]
+            taken += 1
+            held[b] += 1
+        for i in range(want, held[b]):
+            free[end % n_pages] = table[b, i]
+            end += 1
+        held[b] = min(held[b], want)
+        for t in range(n):
+            pos[b, t] = c + t
+            at = (c + t) // page
+            if at < held[b] and 0 <= table[b, at] < n_pages:
+                slot[b, t] = table[b, at] * page + (c + t) % page
+                kv[b, t] = c + t + 1
+    return table, np.array(held), free, np.array([first + taken, end]), pos, slot, kv
+
+
+def tree_sees(parent, n_nodes: int):
+    """parent [T]: [T, T] truth values, node t sees node j: j is t or an ancestor of it."""
+    T = len(parent)
+    sees = np.zeros((T, T), dtype=bool)
+    for t in range(n_nodes):
+        j = t
+        while True:
+            sees[t, j] = True
+            up = int(parent[j])
+            if not 0 <= up < j:
+                break
+            j = up
+    return sees
+
+
+def mask_words(sees):
+    """Truth values over the last axis as 32-bit words, the first in the lowest bit (uint32)."""
+    sees = np.asarray(sees)
+    n = sees.shape[-1]
+    out = np.zeros(sees.shape[:-1] + (-(-n // 32),), dtype=np.uint32)
+    for j in range(n):
+        out[..., j // 32] |= np.where(sees[..., j], np.uint32(1 << (j % 32)), np.uint32(0))
+    return out
+
+
+def seen_attn(q, q_pos, ke, c, seen, W_uk, W_uv, elite_idx, head_dim: int, rope_base: float, d_ck: int = 0):
+    """T queries of ONE sequence over the rows each of them sees (Section 2.1 over the reconstructed keys and values, Section
+    3.2; d_ck > 0: separated latents).  q [T, n_h, d_h]; q_pos [T]; ke [S, n_h, 2r]; c [S, d_c]; seen [T, S] truth values.  Rows
+    that nobody sees are not touched; a query that sees nothing gives zeros."""
+    q, ke, c = (np.asarray(a, dtype=F64) for a in (q, ke, c))
+    W_uk, W_uv, elite_idx = np.asarray(W_uk, dtype=F64), np.asarray(W_uv, dtype=F64), np.asarray(elite_idx)
+    T, n_h, d_h = q.shape
+    r = elite_idx.shape[1]
+    theta = rope_theta(head_dim, rope_base)
+    out = np.zeros_like(q)
+    used = np.flatnonzero(np.asarray(seen).any(axis=0))
+    ke, c, seen = ke[used], c[used], np.asarray(seen)[:, used]
+    c_k, c_v = (c[:, :d_ck], c[:, d_ck:]) if d_ck else (c, c)
+    for h in range(n_h):
+        idx_h = elite_idx[h].astype(np.int64)
+        K = np.concatenate([ke[:, h, :], c_k @ W_uk[:, h, :]], axis=1)
+        V = c_v @ W_uv[:, h, :]
+        for t in range(T):
+            if seen[t].any():
+                q_e = rotate_pairs(q[t, h, elite_dims(idx_h)].reshape(r, 2), F64(int(q_pos[t])) * theta[idx_h]).reshape(2 * r)
+                q_hat = np.concatenate([q_e, q[t, h, nonelite_dims(idx_h, d_h)]])
+                out[t, h] = softmax_attention(q_hat, K[seen[t]], V[seen[t]], d_h)
+    return out
+
+
+# ----------------------------------------------------------------------------------------------
 # RoPElite search (Section 3.1, Algorithm 1): the greedy choice of each head's elite chunks.
 # Round after round, every chunk that is not yet elite is tried as the one additional rotated chunk;
 # the chunk whose scores come closest (L1) to the scores of full RoPE is appended.

@@ -89,6 +89,14 @@ def _load():
                                                  P, I32, I32]),
         "elitekv_mha_decode_workspace_bytes": (SZ, [DP, I64, I64, I32]),
         "elitekv_mha_decode": (C.c_int, [DP, P, P, P, I64, I64, I64, P, P, I64, P, P, SZ, I32, P]),
+        "elitekv_page_plan_workspace_bytes": (SZ, [I64, I64]),
+        "elitekv_page_plan": (C.c_int, [P, P, I64, I64, I32, I32, P, I32, P, P, P, P, P, P, P, P, P, SZ, P]),
+        "elitekv_paged_attn_workspace_bytes": (SZ, [DP, I32, I64, I64, I64, I32]),
+        "elitekv_paged_attn": (C.c_int, [DP, I32, P, P, P, I64, I64, I64, P, I32, I32, P, P, P, P, P, I64, P, P, SZ, I32, P]),
+        "elitekv_tree_plan": (C.c_int, [P, P, P, I64, I64, P, P, P]),
+        "elitekv_tree_attn_workspace_bytes": (SZ, [DP, I32, I64, I64, I64, I32]),
+        "elitekv_tree_attn": (C.c_int, [DP, I32, P, P, P, P, P, I64, I64, I64, I64, P, I32, I32, P, P, P, P, P, I64, P, P, SZ, I32, P]),
+        "elitekv_tree_commit": (C.c_int, [DP, P, P, P, I64, I64, I64, P, I32, I32, P, P, I64, P]),
         "elitekv_stream_read": (C.c_int, [P, SZ, P, P]),
         "elitekv_stream_read_mode": (C.c_int, [P, SZ, P, I32, C.POINTER(SZ), P]),
     }
@@ -450,6 +458,84 @@ def elitekv_decode_attn_stages(dims, q, q_pos, seq_len, max_seq_len, batch_strid
                                          _ptr(out), _ptr(ws), ws_bytes, int(n_splits), _stream(stream), int(stages),
                                          int(d_ck))
     _check(st, "elitekv_decode_attn_stages")
+
+
+TREE_MAX_NODES = 128   # ELITEKV_TREE_MAX_NODES
+
+
+def _cols(block_table):
+    return 0 if block_table is None else int(block_table.shape[1])
+
+
+def elitekv_page_plan_workspace_bytes(B, T) -> int:
+    return _lib.elitekv_page_plan_workspace_bytes(int(B), int(T))
+
+
+def elitekv_page_plan(cached_len, new_len, page_rows, n_pages, block_table, held, held_out, free_pages, free_span,
+                      free_span_out, pos, slot, kv_len, ws, stream=None):
+    """cached_len, new_len, held, held_out [B] int32; block_table [B, cols] int32; free_pages [n_pages] int32;
+    free_span, free_span_out [2] int64; pos, kv_len [B, T] int32, slot [B, T] int64."""
+    B, T = pos.shape
+    ws_bytes = 0 if ws is None else ws.numel() * ws.element_size()
+    st = _lib.elitekv_page_plan(_ptr(cached_len), _ptr(new_len), B, T, int(page_rows), int(n_pages), _ptr(block_table),
+                                _cols(block_table), _ptr(held), _ptr(held_out), _ptr(free_pages), _ptr(free_span),
+                                _ptr(free_span_out), _ptr(pos), _ptr(slot), _ptr(kv_len), _ptr(ws), ws_bytes,
+                                _stream(stream))
+    _check(st, "elitekv_page_plan")
+
+
+def elitekv_paged_attn_workspace_bytes(dims, B, T, max_seq_len, n_splits=0, d_ck=0) -> int:
+    return _lib.elitekv_paged_attn_workspace_bytes(C.byref(dims), int(d_ck), int(B), int(T), int(max_seq_len), int(n_splits))
+
+
+def elitekv_paged_attn(dims, q, q_pos, kv_len, max_seq_len, block_table, page_rows, W_uk, W_uv, elite_idx, ke_plane, c_plane,
+                       out, ws, n_splits=0, d_ck=0, stream=None, plane_rows=None):
+    """q [B, T, n_h, d_h]; q_pos, kv_len [B, T] int32; block_table [B, cols] int32.  d_ck > 0: separated latents."""
+    B, T = q.shape[0], q.shape[1]
+    plane_rows = c_plane.shape[0] if plane_rows is None else plane_rows
+    ws_bytes = 0 if ws is None else ws.numel() * ws.element_size()
+    st = _lib.elitekv_paged_attn(C.byref(dims), int(d_ck), _ptr(q), _ptr(q_pos), _ptr(kv_len), B, T, int(max_seq_len),
+                                 _ptr(block_table), _cols(block_table), int(page_rows), _ptr(W_uk), _ptr(W_uv),
+                                 _ptr(elite_idx), _ptr(ke_plane), _ptr(c_plane), int(plane_rows), _ptr(out), _ptr(ws),
+                                 ws_bytes, int(n_splits), _stream(stream))
+    _check(st, "elitekv_paged_attn")
+
+
+def elitekv_tree_plan(parent, prefix_len, n_nodes, pos, mask, stream=None):
+    """parent, pos [B, T] int32; prefix_len, n_nodes [B] int32; mask [B, T, ceil(T / 32)] int32 (bits)."""
+    B, T = parent.shape
+    st = _lib.elitekv_tree_plan(_ptr(parent), _ptr(prefix_len), _ptr(n_nodes), B, T, _ptr(pos), _ptr(mask), _stream(stream))
+    _check(st, "elitekv_tree_plan")
+
+
+def elitekv_tree_attn_workspace_bytes(dims, B, T, max_seq_len, n_splits=0, d_ck=0) -> int:
+    return _lib.elitekv_tree_attn_workspace_bytes(C.byref(dims), int(d_ck), int(B), int(T), int(max_seq_len), int(n_splits))
+
+
+def elitekv_tree_attn(dims, q, q_pos, prefix_len, n_nodes, mask, max_seq_len, batch_stride_rows, W_uk, W_uv, elite_idx,
+                      ke_plane, c_plane, out, ws, block_table=None, page_rows=0, n_splits=0, d_ck=0, stream=None,
+                      plane_rows=None):
+    """q [B, T, n_h, d_h]; q_pos [B, T], prefix_len, n_nodes [B] int32; mask [B, T, ceil(T / 32)] int32 (bits).
+    block_table [B, cols] int32: a cache in pages (batch_stride_rows is not used then)."""
+    B, T = q.shape[0], q.shape[1]
+    plane_rows = c_plane.shape[0] if plane_rows is None else plane_rows
+    ws_bytes = 0 if ws is None else ws.numel() * ws.element_size()
+    st = _lib.elitekv_tree_attn(C.byref(dims), int(d_ck), _ptr(q), _ptr(q_pos), _ptr(prefix_len), _ptr(n_nodes), _ptr(mask),
+                                B, T, int(max_seq_len), int(batch_stride_rows), _ptr(block_table), _cols(block_table),
+                                int(page_rows), _ptr(W_uk), _ptr(W_uv), _ptr(elite_idx), _ptr(ke_plane), _ptr(c_plane),
+                                int(plane_rows), _ptr(out), _ptr(ws), ws_bytes, int(n_splits), _stream(stream))
+    _check(st, "elitekv_tree_attn")
+
+
+def elitekv_tree_commit(dims, path, path_len, prefix_len, batch_stride_rows, ke_plane, c_plane, block_table=None, page_rows=0,
+                        stream=None, plane_rows=None):
+    """path [B, T] int32: the accepted nodes of every sequence; path_len, prefix_len [B] int32."""
+    B, T = path.shape
+    plane_rows = c_plane.shape[0] if plane_rows is None else plane_rows
+    st = _lib.elitekv_tree_commit(C.byref(dims), _ptr(path), _ptr(path_len), _ptr(prefix_len), B, T, int(batch_stride_rows),
+                                  _ptr(block_table), _cols(block_table), int(page_rows), _ptr(ke_plane), _ptr(c_plane),
+                                  int(plane_rows), _stream(stream))
+    _check(st, "elitekv_tree_commit")
 
 
 def elitekv_mha_decode_workspace_bytes(dims, B, max_seq_len, n_splits=0) -> int:

@@ -68,12 +68,15 @@ __global__ __launch_bounds__(kGenThreads) void qprep_generic_kernel(
 }
 
 // One work-group per (split, head, batch row).  CPT = latent columns per thread.
-template <typename T, int CPT>
+// MAPPED: rows in pages or behind a tree's mask.  A row that is not seen is not read: its weight would be 0, but 0 times what it
+// holds need not be.
+template <typename T, int CPT, bool MAPPED>
 __global__ __launch_bounds__(kGenThreads) void attn_generic_kernel(
     const T* __restrict__ ke_plane, const T* __restrict__ c_plane, const float* __restrict__ qe,
     const float* __restrict__ qt, const int32_t* __restrict__ seq_len, float* __restrict__ part_m,
     float* __restrict__ part_l, float* __restrict__ part_u, int n_h, int two_r, int d_c, int d_q, int d_u,
-    int64_t max_seq_len, int64_t batch_stride_rows, int64_t plane_rows, int n_splits, int chunk, int q_per_seq) {
+    int64_t max_seq_len, int64_t batch_stride_rows, int64_t plane_rows, int n_splits, int chunk, int q_per_seq,
+    RowMap map) {
   extern __shared__ float smem[];
   // a cache row holds d_c latent columns: the first d_q of them enter the scores, the last d_u are
   // accumulated as values (joint latent: d_q = d_u = d_c, the same columns serve both)
@@ -86,10 +89,9 @@ __global__ __launch_bounds__(kGenThreads) void attn_generic_kernel(
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
 
   const int64_t row0 = (int64_t)(b / q_per_seq) * batch_stride_rows;
-  int64_t len = seq_len[b];
-  len = min(len, max_seq_len);
-  len = min(len, plane_rows - row0);
-  len = max(len, (int64_t)0);
+  const int64_t cap = map.table ? max_seq_len : max(min(max_seq_len, plane_rows - row0), (int64_t)0);
+  const SeenRows seen(map, seq_len, b, q_per_seq, batch_stride_rows, cap);
+  const int64_t len = seen.len;
   const int64_t t0 = (int64_t)split * chunk;
   const int64_t t1 = min(t0 + chunk, len);
 
@@ -109,21 +111,23 @@ __global__ __launch_bounds__(kGenThreads) void attn_generic_kernel(
     for (int tt = 0; tt < kGenTile / 4; ++tt) {
       const int ti = wave * (kGenTile / 4) + tt;
       float part = 0.f;
-      if (ti < nt) {
-        const int64_t row = row0 + tile + ti;
+      const bool sees = ti < nt && (!MAPPED || seen.sees(tile + ti));
+      if (sees) {
+        const int64_t row = MAPPED ? seen.row(tile + ti, seen.page(tile + ti)) : row0 + tile + ti;
         const T* crow = c_plane + row * d_c;
         for (int k = lane; k < d_q; k += 64) part = fmaf(qt_s[k], ld(crow, k), part);
         const T* krow = ke_plane + (row * n_h + h) * two_r;
         for (int e = lane; e < two_r; e += 64) part = fmaf(qe_s[e], ld(krow, e), part);
       }
       part = wave_sum(part);
-      if (lane == 0) s_tile[ti] = (ti < nt) ? part : -INFINITY;
+      if (lane == 0) s_tile[ti] = sees ? part : -INFINITY;
     }
     __syncthreads();
     const float sv = s_tile[lane];
     const float m_new = fmaxf(m, wave_max(sv));
-    const float alpha = exp2f(m - m_new);   // m = -inf on the first tile gives 0
-    const float p = exp2f(sv - m_new);      // -inf score gives 0
+    const float m_sub = MAPPED && m_new == -INFINITY ? 0.f : m_new;   // nothing seen yet: weights and sum stay 0
+    const float alpha = exp2f(m - m_sub);   // m = -inf on the first tile gives 0
+    const float p = exp2f(sv - m_sub);      // -inf score gives 0
     l = l * alpha + wave_sum(p);
     if (wave == 0) p_tile[lane] = p;
     __syncthreads();
@@ -132,8 +136,13 @@ __global__ __launch_bounds__(kGenThreads) void attn_generic_kernel(
       const int k = tid + cc * kGenThreads;
       if (k < d_u) {
         float a = acc[cc] * alpha;
-        const T* col = c_plane + (row0 + tile) * d_c + v0 + k;
-        for (int tt = 0; tt < nt; ++tt) a = fmaf(p_tile[tt], ld(col, (int64_t)tt * d_c), a);
+        if constexpr (MAPPED) {
+          for (int tt = 0; tt < nt; ++tt)
+            if (seen.sees(tile + tt)) a = fmaf(p_tile[tt], ld(c_plane + v0 + k, seen.row(tile + tt, seen.page(tile + tt)) * d_c), a);
+        } else {
+          const T* col = c_plane + (row0 + tile) * d_c + v0 + k;
+          for (int tt = 0; tt < nt; ++tt) a = fmaf(p_tile[tt], ld(col, (int64_t)tt * d_c), a);
+        }
         acc[cc] = a;
       }
     }
@@ -235,10 +244,11 @@ static hipError_t launch_decode_generic_t(const DecodeArgs& a, const DecodePlan&
   const dim3 grid(p.n_splits, n_h, (unsigned)a.B);
   const size_t sm = sizeof(float) * (size_t)(d_q + 2 * r + 2 * kGenTile);
   const int cpt = (d_u + kGenThreads - 1) / kGenThreads;
-#define EKV_ATTN(C)                                                                               \
-  attn_generic_kernel<T, C><<<grid, kGenThreads, sm, stream>>>(                                   \
+#define EKV_ATTN_AS(C, MAPPED)                                                                    \
+  attn_generic_kernel<T, C, MAPPED><<<grid, kGenThreads, sm, stream>>>(                           \
       (const T*)a.ke_plane, (const T*)a.c_plane, qe, qt, a.seq_len, pm, pl, pu, n_h, 2 * r, d_c, d_q, d_u, \
-      a.max_seq_len, a.batch_stride_rows, a.plane_rows, p.n_splits, p.chunk, a.q_per_seq)
+      a.max_seq_len, a.batch_stride_rows, a.plane_rows, p.n_splits, p.chunk, a.q_per_seq, a.map)
+#define EKV_ATTN(C) do { if (a.mapped) EKV_ATTN_AS(C, true); else EKV_ATTN_AS(C, false); } while (0)
   if (!(a.stages & 2)) {}
   else if (cpt <= 1) EKV_ATTN(1);
   else if (cpt <= 2) EKV_ATTN(2);
@@ -246,6 +256,7 @@ static hipError_t launch_decode_generic_t(const DecodeArgs& a, const DecodePlan&
   else if (cpt <= 8) EKV_ATTN(8);
   else EKV_ATTN(16);
 #undef EKV_ATTN
+#undef EKV_ATTN_AS
 
   if (!(a.stages & 4)) return hipGetLastError();
   const size_t sm2 = sizeof(float) * (size_t)(d_u + p.n_splits + kGenThreads);

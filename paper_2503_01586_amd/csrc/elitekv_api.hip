@@ -100,7 +100,7 @@ static AutoSplits balanced_splits(int64_t groups, int64_t tiles, int64_t slots) 
 // up-projection's partials in the place of the prepared queries, instead of a piece of their own (the same results; what was
 // there is used up, where otherwise a stage can be repeated)
 static int plan_decode(const elitekv_dims* d, int32_t d_ck, int64_t B, int64_t max_seq, int32_t n_splits,
-                       DecodePlan* p, bool want_fresh = false, bool block = false, bool tight = false) {
+                       DecodePlan* p, bool want_fresh = false, bool block = false, bool tight = false, bool mapped = false) {
   int st = check_dims(d);
   if (st) return st;
   if (B < 0 || max_seq < 0 || n_splits < 0) return ELITEKV_EINVAL;
@@ -126,7 +126,7 @@ static int plan_decode(const elitekv_dims* d, int32_t d_ck, int64_t B, int64_t m
   };
   size_t off = 0;
   p->off_qe = off; off = align_up(off + Bz * nh * 2 * d->r * sizeof(float), 256);
-  if (decode_mfma_supported(*d, d_ck)) {
+  if (!mapped && decode_mfma_supported(*d, d_ck)) {
     // one work-group per (split, group of 32 heads, batch row); one group fills a compute unit
     p->mfma = 1;
     p->head_groups = (d->n_heads + 31) / 32;
@@ -468,6 +468,7 @@ static DecodeArgs decode_args(const elitekv_dims* dims, int32_t d_ck, const void
   a.ws = (char*)ws; a.stages = stages; a.q_per_seq = q_per_seq;
   a.fr_slot = nullptr; a.fr_ke_out = nullptr; a.fr_c_out = nullptr;
   a.no_out_reduce = 0;
+  a.mapped = 0; a.map = RowMap{};
   return a;
 }
 
@@ -476,15 +477,21 @@ static int decode_impl(const elitekv_dims* dims, int32_t d_ck, const void* q, co
                        int64_t batch_stride_rows, const void* W_uk, const void* W_uv,
                        const int32_t* elite_idx, const void* ke_plane, const void* c_plane,
                        int64_t plane_rows, void* out, void* ws, size_t ws_bytes, int32_t n_splits,
-                       void* hip_stream, int32_t stages, int32_t q_per_seq = 1, bool tight = false) {
+                       void* hip_stream, int32_t stages, int32_t q_per_seq = 1, bool tight = false,
+                       const RowMap* map = nullptr) {
   DecodePlan p;
-  int st = plan_decode(dims, d_ck, B, max_seq_len, n_splits, &p, false, false, tight);
+  int st = plan_decode(dims, d_ck, B, max_seq_len, n_splits, &p, false, false, tight, map != nullptr);
   if (st) return st;
   st = decode_check(dims, p, q, q_pos, seq_len, B, batch_stride_rows, W_uk, W_uv, elite_idx, ke_plane, c_plane,
                     plane_rows, out, ws, ws_bytes);
   if (st || B == 0) return st;
-  const DecodeArgs a = decode_args(dims, d_ck, q, q_pos, seq_len, B, max_seq_len, batch_stride_rows, W_uk, W_uv,
-                                   elite_idx, ke_plane, c_plane, plane_rows, out, ws, stages, q_per_seq);
+  DecodeArgs a = decode_args(dims, d_ck, q, q_pos, seq_len, B, max_seq_len, batch_stride_rows, W_uk, W_uv,
+                             elite_idx, ke_plane, c_plane, plane_rows, out, ws, stages, q_per_seq);
+  if (map) {
+    a.mapped = 1;
+    a.map = *map;
+    if (map->table) a.max_seq_len = map->n_pages > 0 ? std::min(max_seq_len, (int64_t)map->cols << map->shift) : 0;
+  }
   const hipError_t e = decode_dispatch(a, p, (hipStream_t)hip_stream);
   return e == hipSuccess ? ELITEKV_OK : ELITEKV_EHIP;
 }
@@ -966,6 +973,129 @@ int elitekv_decode_attn_stages(const elitekv_dims* dims, const void* q, const in
   if (stages < 1 || stages > 7) return ELITEKV_EINVAL;
   return decode_impl(dims, d_ck, q, q_pos, seq_len, B, max_seq_len, batch_stride_rows, W_uk, W_uv, elite_idx,
                      ke_plane, c_plane, plane_rows, out, ws, ws_bytes, n_splits, hip_stream, stages);
+}
+
+/* ---- a cache in pages, trees of drafted tokens ---- */
+
+// Pages of a power of two rows, from a tile of the kernels (16 rows) on.
+static bool page_shift(int32_t page_rows, int32_t* shift) {
+  if (page_rows < 16 || page_rows > (1 << 20) || (page_rows & (page_rows - 1))) return false;
+  *shift = __builtin_ctz((unsigned)page_rows);
+  return true;
+}
+
+// The table of a call's arguments; block_table NULL: rows back to back (and page_rows 0).
+static int page_map(const int32_t* block_table, int32_t table_cols, int32_t page_rows, int64_t plane_rows, RowMap* m) {
+  *m = RowMap{};
+  if (!block_table) return page_rows == 0 ? ELITEKV_OK : ELITEKV_ENULL;
+  if (table_cols < 1 || plane_rows < 0 || !page_shift(page_rows, &m->shift)) return ELITEKV_EINVAL;
+  m->table = block_table;
+  m->cols = table_cols;
+  m->n_pages = (int32_t)std::min<int64_t>(plane_rows >> m->shift, INT32_MAX);
+  return ELITEKV_OK;
+}
+
+size_t elitekv_page_plan_workspace_bytes(int64_t B, int64_t T) {
+  return B > 0 && B <= 65535 && T > 0 && T <= 65536 ? align_up(page_plan_workspace(B), 256) : 0;
+}
+
+int elitekv_page_plan(const int32_t* cached_len, const int32_t* new_len, int64_t B, int64_t T, int32_t page_rows, int32_t n_pages,
+                      int32_t* block_table, int32_t table_cols, const int32_t* held, int32_t* held_out, int32_t* free_pages,
+                      const int64_t* free_span, int64_t* free_span_out, int32_t* pos, int64_t* slot, int32_t* kv_len, void* ws,
+                      size_t ws_bytes, void* hip_stream) {
+  PagePlanArgs a{};
+  if (B < 0 || T < 1 || n_pages < 1 || table_cols < 1 || !page_shift(page_rows, &a.shift)) return ELITEKV_EINVAL;
+  if (B > 65535 || T > 65536) return ELITEKV_EUNSUPPORTED;
+  if (B == 0) return ELITEKV_OK;
+  if (!cached_len || !new_len || !block_table || !held || !held_out || !free_pages || !free_span || !free_span_out || !pos || !slot ||
+      !kv_len || !ws)
+    return ELITEKV_ENULL;
+  if (!aligned16(ws)) return ELITEKV_EALIGN;
+  if (ws_bytes < page_plan_workspace(B)) return ELITEKV_EWORKSPACE;
+  a.cached_len = cached_len; a.new_len = new_len; a.B = B; a.T = (int32_t)T; a.n_pages = n_pages; a.cols = table_cols;
+  a.table = block_table; a.held = held; a.held_out = held_out; a.ring = free_pages; a.span = free_span; a.span_out = free_span_out;
+  a.pos = pos; a.slot = slot; a.kv_len = kv_len; a.ws = ws;
+  return launch_page_plan(a, (hipStream_t)hip_stream) == hipSuccess ? ELITEKV_OK : ELITEKV_EHIP;
+}
+
+size_t elitekv_paged_attn_workspace_bytes(const elitekv_dims* dims, int32_t d_ck, int64_t B, int64_t T, int64_t max_seq_len,
+                                          int32_t n_splits) {
+  DecodePlan p;
+  if (B < 0 || T < 1 || B * T > 65535 || plan_decode(dims, d_ck, B * T, max_seq_len, n_splits, &p, false, false, false, true)) return 0;
+  return p.reserve;
+}
+
+int elitekv_paged_attn(const elitekv_dims* dims, int32_t d_ck, const void* q, const int32_t* q_pos, const int32_t* kv_len, int64_t B,
+                       int64_t T, int64_t max_seq_len, const int32_t* block_table, int32_t table_cols, int32_t page_rows,
+                       const void* W_uk, const void* W_uv, const int32_t* elite_idx, const void* ke_plane, const void* c_plane,
+                       int64_t plane_rows, void* out, void* ws, size_t ws_bytes, int32_t n_splits, void* hip_stream) {
+  int st = check_dims(dims);
+  if (st) return st;
+  if (B < 0 || T < 1) return ELITEKV_EINVAL;
+  if (B > 65535 || T > 65535 || B * T > 65535) return ELITEKV_EUNSUPPORTED;
+  if (B == 0) return ELITEKV_OK;
+  if (!block_table) return ELITEKV_ENULL;
+  RowMap m;
+  st = page_map(block_table, table_cols, page_rows, plane_rows, &m);
+  if (st) return st;
+  return decode_impl(dims, d_ck, q, q_pos, kv_len, B * T, max_seq_len, 0, W_uk, W_uv, elite_idx, ke_plane, c_plane, plane_rows, out, ws,
+                     ws_bytes, n_splits, hip_stream, 7, (int32_t)T, false, &m);
+}
+
+int elitekv_tree_plan(const int32_t* parent, const int32_t* prefix_len, const int32_t* n_nodes, int64_t B, int64_t T, int32_t* pos,
+                      uint32_t* mask, void* hip_stream) {
+  if (B < 0 || T < 1) return ELITEKV_EINVAL;
+  if (B > 65535 || T > ELITEKV_TREE_MAX_NODES) return ELITEKV_EUNSUPPORTED;
+  if (B == 0) return ELITEKV_OK;
+  if (!parent || !prefix_len || !n_nodes || !pos || !mask) return ELITEKV_ENULL;
+  return launch_tree_plan(parent, prefix_len, n_nodes, B, T, pos, mask, (hipStream_t)hip_stream) == hipSuccess ? ELITEKV_OK : ELITEKV_EHIP;
+}
+
+size_t elitekv_tree_attn_workspace_bytes(const elitekv_dims* dims, int32_t d_ck, int64_t B, int64_t T, int64_t max_seq_len,
+                                         int32_t n_splits) {
+  DecodePlan p;
+  if (B < 0 || T < 1 || T > ELITEKV_TREE_MAX_NODES || B * T > 65535 ||
+      plan_decode(dims, d_ck, B * T, max_seq_len, n_splits, &p, false, false, false, true))
+    return 0;
+  return p.reserve;
+}
+
+int elitekv_tree_attn(const elitekv_dims* dims, int32_t d_ck, const void* q, const int32_t* q_pos, const int32_t* prefix_len,
+                      const int32_t* n_nodes, const uint32_t* mask, int64_t B, int64_t T, int64_t max_seq_len,
+                      int64_t batch_stride_rows, const int32_t* block_table, int32_t table_cols, int32_t page_rows, const void* W_uk,
+                      const void* W_uv, const int32_t* elite_idx, const void* ke_plane, const void* c_plane, int64_t plane_rows,
+                      void* out, void* ws, size_t ws_bytes, int32_t n_splits, void* hip_stream) {
+  int st = check_dims(dims);
+  if (st) return st;
+  if (B < 0 || T < 1) return ELITEKV_EINVAL;
+  if (T > ELITEKV_TREE_MAX_NODES || B > 65535 || B * T > 65535) return ELITEKV_EUNSUPPORTED;
+  if (B == 0) return ELITEKV_OK;
+  if (!n_nodes || !mask) return ELITEKV_ENULL;
+  RowMap m;
+  st = page_map(block_table, table_cols, page_rows, plane_rows, &m);
+  if (st) return st;
+  m.nodes = n_nodes; m.mask = mask; m.words = (int32_t)((T + 31) / 32);
+  return decode_impl(dims, d_ck, q, q_pos, prefix_len, B * T, max_seq_len, block_table ? 0 : batch_stride_rows, W_uk, W_uv, elite_idx,
+                     ke_plane, c_plane, plane_rows, out, ws, ws_bytes, n_splits, hip_stream, 7, (int32_t)T, false, &m);
+}
+
+int elitekv_tree_commit(const elitekv_dims* dims, const int32_t* path, const int32_t* path_len, const int32_t* prefix_len, int64_t B,
+                        int64_t T, int64_t batch_stride_rows, const int32_t* block_table, int32_t table_cols, int32_t page_rows,
+                        void* ke_plane, void* c_plane, int64_t plane_rows, void* hip_stream) {
+  int st = check_dims(dims);
+  if (st) return st;
+  if (B < 0 || T < 1 || batch_stride_rows < 0 || plane_rows < 0) return ELITEKV_EINVAL;
+  if (B > 65535 || T > ELITEKV_TREE_MAX_NODES) return ELITEKV_EUNSUPPORTED;
+  if (B == 0) return ELITEKV_OK;
+  if (!path || !path_len || !prefix_len || !c_plane || (dims->r > 0 && !ke_plane)) return ELITEKV_ENULL;
+  if (!aligned16(ke_plane) || !aligned16(c_plane)) return ELITEKV_EALIGN;
+  RowMap m;
+  st = page_map(block_table, table_cols, page_rows, plane_rows, &m);
+  if (st) return st;
+  // rows of a sequence that may be written: its table's, or up to the next sequence's
+  const int64_t cap = block_table ? (int64_t)table_cols << m.shift : batch_stride_rows > 0 ? batch_stride_rows : plane_rows;
+  return launch_tree_commit(*dims, path, path_len, prefix_len, B, T, batch_stride_rows, plane_rows, cap, m, ke_plane, c_plane,
+                            (hipStream_t)hip_stream) == hipSuccess ? ELITEKV_OK : ELITEKV_EHIP;
 }
 
 size_t elitekv_mha_decode_workspace_bytes(const elitekv_dims* dims, int64_t B, int64_t max_seq_len,

@@ -7,6 +7,7 @@
 #include <stdint.h>
 
 #include "../../include/elitekv.h"
+#include "seen_rows.hpp"
 
 namespace ekv {
 
@@ -97,6 +98,10 @@ struct DecodeArgs {
   void* fr_c_out;
   // whole-block step only: the merge leaves its column-chunk partials for the output projection (no out_reduce)
   int32_t no_out_reduce;
+  // a cache in pages, a tree of drafted tokens: where rows lie and which ones a query sees (seen_rows.hpp); max_seq_len then
+  // bounds what the table has room for too.  mapped 0: back to back, the first seq_len[b] of them
+  int32_t mapped;
+  RowMap map;
 };
 
 struct AppendArgs {
@@ -125,6 +130,23 @@ struct AppendArgs {
   // Direct-load GEMM kernels only: zeroed on the way, for a launch behind this one that counts in them
   int* clear = nullptr;
   int32_t n_clear = 0;
+};
+
+struct PagePlanArgs {
+  const int32_t* cached_len;
+  const int32_t* new_len;
+  int64_t B;
+  int32_t T, shift, n_pages, cols;
+  int32_t* table;
+  const int32_t* held;
+  int32_t* held_out;
+  int32_t* ring;
+  const int64_t* span;
+  int64_t* span_out;
+  int32_t* pos;
+  int64_t* slot;
+  int32_t* kv_len;
+  void* ws;
 };
 
 struct MhaArgs {
@@ -200,6 +222,13 @@ size_t search_min_workspace_bytes(int64_t T, int n_h);
 hipError_t launch_ropelite_search(const float* q, const float* k, const int32_t* pos, int64_t T, int n_h, int d_h,
                                   int r, double rope_base, int32_t* elite_out, float* dist_out, char* ws,
                                   size_t ws_bytes, hipStream_t stream);
+size_t page_plan_workspace(int64_t B);
+hipError_t launch_page_plan(const PagePlanArgs& a, hipStream_t stream);
+hipError_t launch_tree_plan(const int32_t* parent, const int32_t* prefix_len, const int32_t* n_nodes, int64_t B, int64_t T,
+                            int32_t* pos, uint32_t* mask, hipStream_t stream);
+hipError_t launch_tree_commit(const elitekv_dims& d, const int32_t* path, const int32_t* path_len, const int32_t* prefix_len,
+                              int64_t B, int64_t T, int64_t stride, int64_t plane_rows, int64_t cap, const RowMap& map,
+                              void* ke_plane, void* c_plane, hipStream_t stream);
 hipError_t launch_stream_read(const void* src, size_t bytes, uint32_t* sink, int mode, size_t* bytes_read,
                               hipStream_t stream);
 
