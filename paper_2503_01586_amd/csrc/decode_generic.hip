@@ -89,7 +89,7 @@ __global__ __launch_bounds__(kGenThreads) void attn_generic_kernel(
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
 
   const int64_t row0 = (int64_t)(b / q_per_seq) * batch_stride_rows;
-  const int64_t cap = map.table ? max_seq_len : max(min(max_seq_len, plane_rows - row0), (int64_t)0);
+  const int64_t cap = map.table ? max_seq_len : min(max_seq_len, plane_rows - row0);
   const SeenRows seen(map, seq_len, b, q_per_seq, batch_stride_rows, cap);
   const int64_t len = seen.len;
   const int64_t t0 = (int64_t)split * chunk;

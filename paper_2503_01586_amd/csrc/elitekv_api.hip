@@ -100,7 +100,7 @@ static AutoSplits balanced_splits(int64_t groups, int64_t tiles, int64_t slots) 
 // up-projection's partials in the place of the prepared queries, instead of a piece of their own (the same results; what was
 // there is used up, where otherwise a stage can be repeated)
 static int plan_decode(const elitekv_dims* d, int32_t d_ck, int64_t B, int64_t max_seq, int32_t n_splits,
-                       DecodePlan* p, bool want_fresh = false, bool block = false, bool tight = false, bool mapped = false) {
+                       DecodePlan* p, bool want_fresh = false, bool block = false, bool tight = false) {
   int st = check_dims(d);
   if (st) return st;
   if (B < 0 || max_seq < 0 || n_splits < 0) return ELITEKV_EINVAL;
@@ -126,7 +126,7 @@ static int plan_decode(const elitekv_dims* d, int32_t d_ck, int64_t B, int64_t m
   };
   size_t off = 0;
   p->off_qe = off; off = align_up(off + Bz * nh * 2 * d->r * sizeof(float), 256);
-  if (!mapped && decode_mfma_supported(*d, d_ck)) {
+  if (decode_mfma_supported(*d, d_ck)) {
     // one work-group per (split, group of 32 heads, batch row); one group fills a compute unit
     p->mfma = 1;
     p->head_groups = (d->n_heads + 31) / 32;
@@ -480,7 +480,7 @@ static int decode_impl(const elitekv_dims* dims, int32_t d_ck, const void* q, co
                        void* hip_stream, int32_t stages, int32_t q_per_seq = 1, bool tight = false,
                        const RowMap* map = nullptr) {
   DecodePlan p;
-  int st = plan_decode(dims, d_ck, B, max_seq_len, n_splits, &p, false, false, tight, map != nullptr);
+  int st = plan_decode(dims, d_ck, B, max_seq_len, n_splits, &p, false, false, tight);
   if (st) return st;
   st = decode_check(dims, p, q, q_pos, seq_len, B, batch_stride_rows, W_uk, W_uv, elite_idx, ke_plane, c_plane,
                     plane_rows, out, ws, ws_bytes);
@@ -490,7 +490,7 @@ static int decode_impl(const elitekv_dims* dims, int32_t d_ck, const void* q, co
   if (map) {
     a.mapped = 1;
     a.map = *map;
-    if (map->table) a.max_seq_len = map->n_pages > 0 ? std::min(max_seq_len, (int64_t)map->cols << map->shift) : 0;
+    if (map->table && map->n_pages == 0) a.max_seq_len = 0;
   }
   const hipError_t e = decode_dispatch(a, p, (hipStream_t)hip_stream);
   return e == hipSuccess ? ELITEKV_OK : ELITEKV_EHIP;
@@ -1018,11 +1018,31 @@ int elitekv_page_plan(const int32_t* cached_len, const int32_t* new_len, int64_t
   return launch_page_plan(a, (hipStream_t)hip_stream) == hipSuccess ? ELITEKV_OK : ELITEKV_EHIP;
 }
 
+// Many queries per sequence: the rows are gathered from their pages into planes of the workspace, then elitekv_prefill_attn's
+// kernels run on these.  Workspace: [elite keys | latents | theirs].
+struct PagedPrompt { size_t off_c, off_flash; };
+static PagedPrompt paged_prompt(const elitekv_dims* d, int64_t B, int64_t S) {
+  PagedPrompt l;
+  l.off_c = align_up((size_t)(B * S) * 2 * d->r * d->n_heads * elem_bytes(d), 256);
+  l.off_flash = align_up(l.off_c + (size_t)(B * S) * d->d_c * elem_bytes(d), 256);
+  return l;
+}
+constexpr int64_t kPromptRows = 64;       // up to so many rows every query is absorbed (prefill_flash_supported)
+static bool paged_prompt_fits(const elitekv_dims* d, int64_t B, int64_t T) {
+  return B * T <= (1LL << 24) && B * d->n_heads <= (1 << 20);
+}
+
 size_t elitekv_paged_attn_workspace_bytes(const elitekv_dims* dims, int32_t d_ck, int64_t B, int64_t T, int64_t max_seq_len,
                                           int32_t n_splits) {
+  if (check_dims(dims) || B < 0 || B > 65535 || T < 1 || T > (1 << 24) || max_seq_len < 0 || d_ck < 0 || d_ck >= dims->d_c) return 0;
   DecodePlan p;
-  if (B < 0 || T < 1 || B * T > 65535 || plan_decode(dims, d_ck, B * T, max_seq_len, n_splits, &p, false, false, false, true)) return 0;
-  return p.reserve;
+  if (prefill_flash_supported(*dims, d_ck, T, max_seq_len)) {
+    if (!paged_prompt_fits(dims, B, T)) return 0;
+    // (and room for a shorter bound, with which the queries are absorbed)
+    const size_t absorbed = B * T <= 65535 && plan_decode(dims, d_ck, B * T, kPromptRows, n_splits, &p) == ELITEKV_OK ? p.reserve : 0;
+    return std::max(paged_prompt(dims, B, max_seq_len).off_flash + prefill_flash_workspace(*dims, B, max_seq_len), absorbed);
+  }
+  return B * T > 65535 || plan_decode(dims, d_ck, B * T, max_seq_len, n_splits, &p) ? 0 : p.reserve;
 }
 
 int elitekv_paged_attn(const elitekv_dims* dims, int32_t d_ck, const void* q, const int32_t* q_pos, const int32_t* kv_len, int64_t B,
@@ -1031,15 +1051,34 @@ int elitekv_paged_attn(const elitekv_dims* dims, int32_t d_ck, const void* q, co
                        int64_t plane_rows, void* out, void* ws, size_t ws_bytes, int32_t n_splits, void* hip_stream) {
   int st = check_dims(dims);
   if (st) return st;
-  if (B < 0 || T < 1) return ELITEKV_EINVAL;
-  if (B > 65535 || T > 65535 || B * T > 65535) return ELITEKV_EUNSUPPORTED;
+  if (B < 0 || T < 1 || max_seq_len < 0 || n_splits < 0 || d_ck < 0 || d_ck >= dims->d_c) return ELITEKV_EINVAL;
+  if (B > 65535 || T > (1 << 24)) return ELITEKV_EUNSUPPORTED;
   if (B == 0) return ELITEKV_OK;
   if (!block_table) return ELITEKV_ENULL;
   RowMap m;
   st = page_map(block_table, table_cols, page_rows, plane_rows, &m);
   if (st) return st;
-  return decode_impl(dims, d_ck, q, q_pos, kv_len, B * T, max_seq_len, 0, W_uk, W_uv, elite_idx, ke_plane, c_plane, plane_rows, out, ws,
-                     ws_bytes, n_splits, hip_stream, 7, (int32_t)T, false, &m);
+  const int64_t S = std::min(max_seq_len, (int64_t)table_cols << m.shift);
+  if (m.n_pages > 0 && n_splits <= kMaxSplits && prefill_flash_supported(*dims, d_ck, T, S)) {
+    if (!paged_prompt_fits(dims, B, T)) return ELITEKV_EUNSUPPORTED;
+    if (!q || !q_pos || !kv_len || !W_uk || !W_uv || !elite_idx || !ke_plane || !c_plane || !out || !ws) return ELITEKV_ENULL;
+    if (!aligned16(q) || !aligned16(W_uk) || !aligned16(W_uv) || !aligned16(ke_plane) || !aligned16(c_plane) || !aligned16(out) ||
+        !aligned16(ws))
+      return ELITEKV_EALIGN;
+    const PagedPrompt l = paged_prompt(dims, B, S);
+    if (ws_bytes < l.off_flash + prefill_flash_min_workspace(*dims, B, S)) return ELITEKV_EWORKSPACE;
+    char* w = (char*)ws;
+    const hipStream_t stream = (hipStream_t)hip_stream;
+    hipError_t e = launch_gather_pages(*dims, m, ke_plane, c_plane, B, S, w, w + l.off_c, stream);
+    if (e != hipSuccess) return ELITEKV_EHIP;
+    const DecodeArgs a = decode_args(dims, d_ck, q, q_pos, kv_len, B * T, S, S, W_uk, W_uv, elite_idx, w, w + l.off_c, B * S, out,
+                                     w + l.off_flash, 7, (int32_t)T);
+    e = launch_prefill_flash(a, B, T, ws_bytes - l.off_flash, stream);
+    return e == hipSuccess ? ELITEKV_OK : ELITEKV_EHIP;
+  }
+  if (B * T > 65535) return ELITEKV_EUNSUPPORTED;
+  return decode_impl(dims, d_ck, q, q_pos, kv_len, B * T, S, 0, W_uk, W_uv, elite_idx, ke_plane, c_plane, plane_rows, out, ws, ws_bytes,
+                     n_splits, hip_stream, 7, (int32_t)T, false, &m);
 }
 
 int elitekv_tree_plan(const int32_t* parent, const int32_t* prefix_len, const int32_t* n_nodes, int64_t B, int64_t T, int32_t* pos,
@@ -1055,7 +1094,7 @@ size_t elitekv_tree_attn_workspace_bytes(const elitekv_dims* dims, int32_t d_ck,
                                          int32_t n_splits) {
   DecodePlan p;
   if (B < 0 || T < 1 || T > ELITEKV_TREE_MAX_NODES || B * T > 65535 ||
-      plan_decode(dims, d_ck, B * T, max_seq_len, n_splits, &p, false, false, false, true))
+      plan_decode(dims, d_ck, B * T, max_seq_len, n_splits, &p))
     return 0;
   return p.reserve;
 }
@@ -1075,6 +1114,7 @@ int elitekv_tree_attn(const elitekv_dims* dims, int32_t d_ck, const void* q, con
   st = page_map(block_table, table_cols, page_rows, plane_rows, &m);
   if (st) return st;
   m.nodes = n_nodes; m.mask = mask; m.words = (int32_t)((T + 31) / 32);
+  if (block_table) max_seq_len = std::min(max_seq_len, (int64_t)table_cols << m.shift);
   return decode_impl(dims, d_ck, q, q_pos, prefix_len, B * T, max_seq_len, block_table ? 0 : batch_stride_rows, W_uk, W_uv, elite_idx,
                      ke_plane, c_plane, plane_rows, out, ws, ws_bytes, n_splits, hip_stream, 7, (int32_t)T, false, &m);
 }

@@ -224,6 +224,8 @@ hipError_t launch_ropelite_search(const float* q, const float* k, const int32_t*
                                   size_t ws_bytes, hipStream_t stream);
 size_t page_plan_workspace(int64_t B);
 hipError_t launch_page_plan(const PagePlanArgs& a, hipStream_t stream);
+hipError_t launch_gather_pages(const elitekv_dims& d, const RowMap& map, const void* ke_plane, const void* c_plane, int64_t B, int64_t S,
+                               void* ke_out, void* c_out, hipStream_t stream);
 hipError_t launch_tree_plan(const int32_t* parent, const int32_t* prefix_len, const int32_t* n_nodes, int64_t B, int64_t T,
                             int32_t* pos, uint32_t* mask, hipStream_t stream);
 hipError_t launch_tree_commit(const elitekv_dims& d, const int32_t* path, const int32_t* path_len, const int32_t* prefix_len,

@@ -154,6 +154,41 @@ hipError_t launch_page_plan(const PagePlanArgs& a, hipStream_t stream) {
   return hipGetLastError();
 }
 
+// ---- a prompt's rows ----
+// The first S rows of every sequence, from its pages to planes in which they lie back to back: what the rebuild of keys and values for
+// many queries reads (elitekv_prefill_attn's kernels).  A work-group copies a tile of sixteen rows, which lies inside one page, of both
+// planes.
+// TODO-FIGURES
+__global__ __launch_bounds__(256) void gather_pages_kernel(const RowMap map, const ekv_u32x4* __restrict__ ke_plane,
+                                                           const ekv_u32x4* __restrict__ c_plane, int ke_units, int c_units, int64_t S,
+                                                           ekv_u32x4* __restrict__ ke_out, ekv_u32x4* __restrict__ c_out) {
+  const int64_t b = blockIdx.y, j = (int64_t)blockIdx.x * 16, to = b * S + j;
+  const int rows = (int)min((int64_t)16, S - j);
+  const int page = uniform_load(map.table + b * map.cols + (j >> map.shift));
+  const int64_t from = ((int64_t)((uint32_t)page < (uint32_t)map.n_pages ? page : 0) << map.shift) + (j & ((1 << map.shift) - 1));
+  auto copy = [&](const ekv_u32x4* src, ekv_u32x4* dst, int n) {
+    int i = threadIdx.x;
+    for (; i + 3 * 256 < n; i += 4 * 256) {                // four pieces under way
+      ekv_u32x4 v[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) v[u] = src[i + u * 256];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) dst[i + u * 256] = v[u];
+    }
+    for (; i < n; i += 256) dst[i] = src[i];
+  };
+  copy(c_plane + from * c_units, c_out + to * c_units, rows * c_units);
+  copy(ke_plane + from * ke_units, ke_out + to * ke_units, rows * ke_units);
+}
+
+hipError_t launch_gather_pages(const elitekv_dims& d, const RowMap& map, const void* ke_plane, const void* c_plane, int64_t B, int64_t S,
+                               void* ke_out, void* c_out, hipStream_t stream) {
+  gather_pages_kernel<<<dim3((unsigned)((S + 15) / 16), (unsigned)B), 256, 0, stream>>>(
+      map, (const ekv_u32x4*)ke_plane, (const ekv_u32x4*)c_plane, 2 * d.r * d.n_heads * 2 / 16, d.d_c * 2 / 16, S, (ekv_u32x4*)ke_out,
+      (ekv_u32x4*)c_out);
+  return hipGetLastError();
+}
+
 // ---- trees ----
 // A work-group per sequence, a thread per node.  A node sees itself and what its parent sees: the masks and the nodes that the
 // chains have reached double in every round (mask |= the reached node's mask), seven rounds for a chain of 128; the depth is the

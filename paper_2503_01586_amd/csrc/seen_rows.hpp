@@ -40,23 +40,27 @@ EKV_ROWS_FN T uniform_load(const T* p) {
 }
 
 struct SeenRows {
-  const int32_t* table;                     // the sequence's row of the table
+  const int32_t* table;                     // the sequence's row of the table; without one, something that may be read, and a shift that
+  bool paged;                               // has every row on "page" 0 (a page is looked up without a branch, which would split the
+                                            // loop of the matrix-core kernels: their accumulators then leave the accumulation registers)
   const uint32_t* mask;                     // the query's row of the masks
-  int64_t prefix, len;                      // rows ahead of the tree; one past the last row that is seen (0: nothing is)
+  int prefix, len;                          // rows ahead of the tree; one past the last row that is seen (0: nothing is)
   int64_t row0;                             // rows back to back: the sequence's first
   int shift, n_pages, words;
 
   // seq_len: of every query, or the rows ahead of every sequence's tree; cap: rows of a sequence that may be read at all
-  EKV_ROWS_FN SeenRows(const RowMap& m, const int32_t* seq_len, int b, int q_per_seq, int64_t stride, int64_t cap) {
+  EKV_ROWS_FN SeenRows(const RowMap& m, const int32_t* seq_len, int b, int q_per_seq, int64_t stride, int64_t cap64) {
     const int seq = b / q_per_seq, t = b - seq * q_per_seq;
-    shift = m.shift; n_pages = m.n_pages; words = m.words;
+    const int cap = (int)max(min(cap64, (int64_t)(INT32_MAX - 256)), (int64_t)0);    // (room for sums of a row and a tile or a tree)
+    paged = m.table != nullptr;
+    shift = paged ? m.shift : 31; n_pages = m.n_pages; words = m.words;
     row0 = seq * stride;
-    table = m.table ? m.table + (int64_t)seq * m.cols : nullptr;
+    table = paged ? m.table + (int64_t)seq * m.cols : seq_len;
     mask = m.nodes ? m.mask + ((int64_t)seq * q_per_seq + t) * m.words : nullptr;
-    prefix = len = min(max((int64_t)uniform_load(seq_len + (mask ? seq : b)), (int64_t)0), cap);
+    prefix = len = min(max(uniform_load(seq_len + (mask ? seq : b)), 0), cap);
     if (mask) {
       const int nodes = min(uniform_load(m.nodes + seq), q_per_seq);
-      const int room = (int)min((int64_t)nodes, cap - prefix);   // drafted tokens whose rows may be read
+      const int room = min(nodes, cap - prefix);                 // drafted tokens whose rows may be read
       for (int w = 0; w < words; ++w) {
         uint32_t bits = uniform_load(mask + w);
         if (room < 32 * w + 32) bits = room > 32 * w ? bits & ((1u << (room - 32 * w)) - 1u) : 0u;
@@ -67,20 +71,19 @@ struct SeenRows {
   }
 
   // the page of a tile that begins at row j < len
-  EKV_ROWS_FN int page(int64_t j) const { return table ? uniform_load(table + (int)(j >> shift)) : 0; }
+  EKV_ROWS_FN int page(int j) const { return uniform_load(table + (j >> shift)); }
   // the plane row of row j, whose page that is
-  EKV_ROWS_FN int64_t row(int64_t j, int page) const {
-    if (!table) return row0 + j;
-    const int64_t p = (uint32_t)page < (uint32_t)n_pages ? page : 0;
-    return (p << shift) + (j & ((1 << shift) - 1));
+  EKV_ROWS_FN int64_t row(int j, int page) const {
+    if (!paged) return row0 + j;
+    const int p = (uint32_t)page < (uint32_t)n_pages ? page : 0;
+    return ((int64_t)p << shift) + (j & ((1 << shift) - 1));
   }
 
   // which of the rows j .. j + 15 are seen (j < len): bit i for row j + i
-  EKV_ROWS_FN uint32_t tile(int64_t j) const {
-    const int64_t left = len - j;
-    uint32_t seen = left >= 16 ? 0xffffu : (1u << (int)left) - 1u;
+  EKV_ROWS_FN uint32_t tile(int j) const {
+    uint32_t seen = len - j >= 16 ? 0xffffu : (1u << (len - j)) - 1u;
     if (mask && j + 16 > prefix) {
-      const int node = (int)(j - prefix), lo = max(node, 0), w = lo >> 5;    // (-15 at least)
+      const int node = j - prefix, lo = max(node, 0), w = lo >> 5;           // (-15 at least)
       uint64_t bits = w < words ? uniform_load(mask + w) : 0u;
       if (w + 1 < words) bits |= (uint64_t)uniform_load(mask + w + 1) << 32;
       bits >>= lo & 31;
@@ -89,11 +92,10 @@ struct SeenRows {
     }
     return seen;
   }
-  EKV_ROWS_FN bool sees(int64_t j) const {
+  EKV_ROWS_FN bool sees(int j) const {
     if (j >= len) return false;
     if (!mask || j < prefix) return true;
-    const int node = (int)(j - prefix);
-    return (mask[node >> 5] >> (node & 31)) & 1u;
+    return (mask[(j - prefix) >> 5] >> ((j - prefix) & 31)) & 1u;
   }
 };
 

@@ -301,7 +301,7 @@ __global__ __launch_bounds__(kTtWaves * 64) void attn_tiled_kernel(
   const int head_ld = min(head, n_h - 1);                 // lanes past the last head repeat it and store nothing
 
   const int64_t row0 = (int64_t)(b / q_per_seq) * batch_stride_rows;
-  const int64_t cap = map.table ? max_seq_len : max(min(max_seq_len, plane_rows - row0), (int64_t)0);
+  const int64_t cap = map.table ? max_seq_len : min(max_seq_len, plane_rows - row0);
   const SeenRows seen(map, seq_len, b, q_per_seq, batch_stride_rows, cap);
   const int64_t len = seen.len;
   const int64_t n_tiles = (len + kTtTok - 1) / kTtTok;

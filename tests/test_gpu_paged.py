@@ -166,6 +166,39 @@ def test_lengths_past_the_table_and_the_bound_are_cut(name):
     assert np.all(got[1] == 0.0)
 
 
+PROMPTS = {
+    "7b": (shape(64, 32, 128, 8, 1536, "bf16"), 0),
+    "r4": (shape(64, 16, 128, 4, 256, "bf16"), 0),
+    "slrd": (shape(64, 16, 128, 8, 1536, "bf16"), 768),
+}
+
+
+@pytest.mark.parametrize("page", [16, 128])
+@pytest.mark.parametrize("name", list(PROMPTS))
+def test_prompts_over_pages(name, page, monkeypatch):
+    """Many queries per sequence: rows gathered, keys and values rebuilt.  The same workspace then serves a bound of few rows, whose
+    queries are absorbed, and a table too short for the bound."""
+    print("prompts", name, page, flush=True)
+    monkeypatch.setitem(SHAPES, name, PROMPTS[name])
+    lens, T = [300, 61, 190], 70
+    k = Cache(name, lens, page, seed=41)
+    assert ekv.elitekv_prefill_plan(k.dims, 3, T, 300, 1 << 40, d_ck=k.d_ck) != ekv.PREFILL_ABSORBED
+    q = k.queries(T)
+    kv = np.array([[max(n - T + t + 1, 0) for t in range(T)] for n in lens])
+    pos = np.maximum(kv - 1, 0)
+    seen = lambda cut: [np.arange(n)[None] < np.minimum(kv[b], cut)[:, None] for b, n in enumerate(lens)]
+    ws = torch.full((ekv.elitekv_paged_attn_workspace_bytes(k.dims, 3, T, 333, 0, k.d_ck),), 0xFF, dtype=torch.uint8, device=DEV)
+    got = host64(k.paged(q, pos, kv, max_seq=333, ws=ws))
+    _close("%s page %d" % (name, page), got, k.reference(q, pos, seen(333)), k.dt)
+    assert np.all(got[kv == 0] == 0.0)
+    got = host64(k.paged(q, pos, kv, max_seq=50, ws=ws))
+    _close("%s page %d, 50 rows" % (name, page), got, k.reference(q, pos, seen(50)), k.dt)
+    k.table = np.ascontiguousarray(k.table[:, :-(-200 // page)])
+    cut = k.table.shape[1] * page
+    got = host64(k.paged(q, pos, kv, max_seq=333, ws=ws))
+    _close("%s page %d, short table" % (name, page), got, k.reference(q, pos, seen(cut)), k.dt)
+
+
 def test_pages_in_order_give_the_bits_of_the_rows_back_to_back():
     sh, _ = SHAPES["7b"]
     lens, stride = [300, 129], 320

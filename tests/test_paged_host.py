@@ -52,7 +52,7 @@ def test_paged_attn_refusals(shape):
     for bad in (dict(B=-1), dict(T=0), dict(page=0), dict(page=17), dict(page=24), dict(cols=0), dict(cols=-1), dict(rows=-1),
                 dict(max_seq=-1), dict(ns=-1), dict(d_ck=d.d_c), dict(d_ck=-1)):
         assert _paged(d, **bad) == ekv.EINVAL, bad
-    for bad in (dict(B=300, T=300), dict(B=1 << 40, T=1 << 40), dict(ns=4096)):
+    for bad in (dict(B=300, T=300, max_seq=60), dict(B=1 << 40, T=1 << 40), dict(T=(1 << 24) + 1), dict(ns=4096)):
         assert _paged(d, **bad) == ekv.EUNSUPPORTED, bad
     for k in ("q", "q_pos", "kv", "table", "W_uk", "W_uv", "idx", "ke", "c", "out", "ws"):
         assert _paged(d, **{k: None}) == ekv.ENULL, k
@@ -64,7 +64,24 @@ def test_paged_attn_refusals(shape):
         sizes = [ekv.elitekv_paged_attn_workspace_bytes(d, 2, 3, s, d_ck=d_ck) for s in (1, 16, 100, 128, 5000)]
         assert sizes == sorted(sizes) and sizes[0] > 0
     assert ekv.elitekv_paged_attn_workspace_bytes(d, 2, 0, 128) == 0
-    assert ekv.elitekv_paged_attn_workspace_bytes(d, 300, 300, 128) == 0
+    assert ekv.elitekv_paged_attn_workspace_bytes(d, 300, 300, 60) == 0
+
+
+def test_prompt_workspaces():
+    """Many queries: room for the gathered rows and what the prefill's kernels need; a size serves every shorter bound."""
+    d = ekv.make_dims(64, 32, 128, 8, 1536, "bf16")
+    for d_ck in (0, 768):
+        sizes = [ekv.elitekv_paged_attn_workspace_bytes(d, 2, 100, s, d_ck=d_ck) for s in (1, 64, 65, 100, 512, 513, 4000)]
+        assert sizes == sorted(sizes)
+        need = 2 * 4000 * (2 * 8 * 32 + 1536) * 2 + 2 * 4000 * 32 * 240 * 2
+        assert need <= sizes[-1]
+        small = dict(B=2, T=100, max_seq=4000, cols=63, page=64, rows=1 << 20, d_ck=d_ck)
+        assert _paged(d, **small, wsb=need - 1) == ekv.EWORKSPACE
+        for k in ("q", "q_pos", "kv", "table", "W_uk", "W_uv", "idx", "ke", "c", "out", "ws"):
+            assert _paged(d, **{**small, k: None}) == ekv.ENULL, k
+        for k in ("q", "W_uk", "W_uv", "ke", "c", "out", "ws"):
+            assert _paged(d, **{**small, k: FAKE + 8}) == ekv.EALIGN, k
+    assert _paged(d, B=60000, T=1000, max_seq=4000, cols=63, page=64) == ekv.EUNSUPPORTED
 
 
 def _tree(d, **kw):
