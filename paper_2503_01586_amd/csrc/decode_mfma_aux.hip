@@ -5,6 +5,8 @@
 //                  up-projection of a chunk of latent columns (Section 3.2, B^v_J), one batch row
 //                  (the version for a batch is merge_mfma.hip)
 //                  the last work-group of a head to finish adds the chunks' partials (chunk_sum.hpp)
+#include <algorithm>
+
 #include "common.hpp"
 #include "chunk_sum.hpp"
 #include "launch.hpp"
@@ -46,7 +48,19 @@ static hipError_t launch_qprep_bt(const DecodeArgs& a, const DecodePlan& p, floa
 template <int KS>
 __global__ __launch_bounds__(256) void qprep_mfma_kernel(const QprepRowsParams P, const RopeTable rope) {
   extern __shared__ __attribute__((aligned(16))) char qms[];
-  qprep_mfma_body<KS>(P, rope, blockIdx.x, blockIdx.y, qms);
+  qprep_mfma_body<KS>(P, rope, blockIdx.x, blockIdx.y, 0, P.B, qms);
+}
+
+// Many rows (drafted trees): a work-group takes `rows` of them (a multiple of kQmRows), and the heads of one block of columns and rows
+// run on one XCD, one after the other: a KiB of the operand layout holds 16 heads, and pieces of 16 bytes from eight L2s go to
+// memory one by one.  TODO-FIGURES
+template <int KS>
+__global__ __launch_bounds__(256) void qprep_many_kernel(const QprepRowsParams P, const RopeTable rope, int rows, int col_blocks, int blocks) {
+  extern __shared__ __attribute__((aligned(16))) char qms[];
+  const int slot = blockIdx.x >> 3, block = slot / P.n_h * 8 + (blockIdx.x & 7);
+  if (block >= blocks) return;
+  const int b0 = block / col_blocks * rows;
+  qprep_mfma_body<KS, true>(P, rope, block % col_blocks, slot % P.n_h, b0, min(P.B, b0 + rows), qms);
 }
 
 bool qprep_mfma_supported(const elitekv_dims& d, int d_q, int64_t B) {
@@ -60,9 +74,16 @@ static hipError_t launch_qprep_mfma(const DecodeArgs& a, const DecodePlan& p, fl
   const int ks = (nd + 15) / 16;
   const size_t sm = qprep_mfma_lds(d.head_dim, d.r);
   const dim3 grid((p.d_q + 127) / 128, d.n_heads);
+  // several passes of rows: as many work-groups as the chip holds at once share them, each reads its piece of W_uk again (from the L2)
+  const int passes = (int)((a.B + kQmRows - 1) / kQmRows), parts = std::min(passes, std::max(1, 1024 / (int)(grid.x * grid.y)));
+  const int rows = (passes + parts - 1) / parts * kQmRows, blocks = (int)grid.x * (int)((a.B + rows - 1) / rows);
   const QprepRowsParams P = make_qprep_rows_params(a, p, qe, qt);
   const RopeTable rope = rope_table(d.rope_base, d.head_dim);
-#define EKV_QM(KSV) qprep_mfma_kernel<KSV><<<grid, 256, sm, stream>>>(P, rope)
+#define EKV_QM(KSV)                                                                                                              \
+  if (rows < a.B)                                                                                                                \
+    qprep_many_kernel<KSV><<<(blocks + 7) / 8 * 8 * d.n_heads, 256, sm, stream>>>(P, rope, rows, (int)grid.x, blocks);          \
+  else                                                                                                                           \
+    qprep_mfma_kernel<KSV><<<grid, 256, sm, stream>>>(P, rope)
   switch (ks) {
     case 1: EKV_QM(1); break;
     case 2: EKV_QM(2); break;
@@ -276,6 +297,7 @@ int merge_up_width(int n_heads, int d_u) {
 
 hipError_t launch_merge_up(const DecodeArgs& a, const DecodePlan& p, hipStream_t stream) {
   const elitekv_dims& d = a.dims;
+  if (merge_rows_pays(a, p)) return launch_merge_rows(a, p, stream);
   if (p.merge_batch) {
     hipError_t e = launch_merge_mfma(a, p, stream);
     if (e != hipSuccess || a.no_out_reduce) return e;

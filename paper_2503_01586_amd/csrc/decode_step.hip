@@ -189,7 +189,7 @@ __global__ __launch_bounds__(256) void decode_front_mfma_kernel(const AppendSkin
   extern __shared__ __attribute__((aligned(16))) char fsm[];
   const int wg = blockIdx.x;
   if (wg < n_qprep) {
-    qprep_mfma_body<KS>(Q, rope, wg % q_blocks, wg / q_blocks, fsm);          // (block of 128 latent columns, head)
+    qprep_mfma_body<KS>(Q, rope, wg % q_blocks, wg / q_blocks, 0, Q.B, fsm);    // (block of 128 latent columns, head)
   } else {
     const int e = wg - n_qprep;
     append_skinny_body<TT>(A, e % n_blocks, e / n_blocks, fsm);               // (column block, contraction split)

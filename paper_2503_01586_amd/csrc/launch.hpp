@@ -205,6 +205,8 @@ bool decode_front_mfma_plan(const elitekv_dims& d, int d_ck, int d_q, int64_t B,
 hipError_t launch_decode_front_mfma(const AppendArgs& ap, const DecodeArgs& a, const DecodePlan& p, hipStream_t stream);
 bool merge_mfma_supported(const elitekv_dims& d, int d_u, int64_t B);
 hipError_t launch_merge_mfma(const DecodeArgs& a, const DecodePlan& p, hipStream_t stream);
+bool merge_rows_pays(const DecodeArgs& a, const DecodePlan& p);      // many rows: the sum over the latent columns in one launch
+hipError_t launch_merge_rows(const DecodeArgs& a, const DecodePlan& p, hipStream_t stream);
 int merge_up_width(int n_heads, int d_u);     // latent columns per work-group of the one-row merge; 0: the batched merge
 hipError_t launch_merge_up(const DecodeArgs& a, const DecodePlan& p, hipStream_t stream);
 hipError_t launch_decode_mfma(const DecodeArgs& a, const DecodePlan& p, hipStream_t stream);

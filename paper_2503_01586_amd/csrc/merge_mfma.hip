@@ -267,6 +267,133 @@ __global__ __launch_bounds__(256) void merge_up_mfma_kernel(
   }
 }
 
+// The same for many rows of up to four splits (trees of drafted tokens): work-group <-> (head, 64 rows), every stage of 128 latent
+// columns one after the other, so that the up-projection's sum stays in the accumulators instead of a partial per stage in memory (512
+// rows of 32 heads and 768 columns: 50 MB written, and read again by out_reduce).  The arithmetic of merge_up_mfma_kernel: merged,
+// normalised latents in fp32, as bf16 high part + remainder.  The two parts lie in LDS, [64 rows][128 columns] each, so that sixteen lanes
+// read 256 bytes of one row of the accumulators (a lane per row, as the operand of the product would have it, touches 32 pages of memory
+// with every load: 38 us instead of TODO for 512 rows); a stage's loads are requested while the stage before is multiplied.
+// TODO-FIGURES
+constexpr int kMrThreads = 256, kMrRows = 64, kMrSplits = 4;
+constexpr int kMrURow = kMmCols * 2 + 16;                   // bytes of a row of a part in LDS (padded)
+
+template <int DH, int NP>
+__global__ __launch_bounds__(kMrThreads) void merge_rows_kernel(const float* __restrict__ part_m, const float* __restrict__ part_l,
+                                                                const bf16_t* __restrict__ part_u, const bf16_t* __restrict__ W_uv,
+                                                                bf16_t* __restrict__ out, int B, int n_h, int nhp, int d_u) {
+  constexpr int WROW = MergeMfmaLayout<DH>::WROW, NT = DH / 64, KS = kMmCols / 16;
+  extern __shared__ __attribute__((aligned(16))) char msm3[];
+  char* wst = msm3;                                        // [128 k][WROW]
+  char* ust = msm3 + kMmCols * WROW;                       // high parts [64][kMrURow], remainders behind them
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int head = blockIdx.x, b0 = blockIdx.y * kMrRows;
+  const int n32 = lane & 31, hi = lane >> 5, i16 = lane & 15, q16 = lane >> 4;
+
+  constexpr int CPR = DH / 8, WPASS = kMmCols * CPR / kMrThreads, UPASS = kMrRows * 16 / kMrThreads;
+  const int cl = tid & 15, r0 = tid >> 4;                  // this thread's 16 bytes of rows r0, r0 + 16, ...
+  uint4 wld[WPASS], uld[UPASS][NP];
+  const bf16_t* ub[UPASS];
+  float scale[UPASS][NP];
+#pragma unroll
+  for (int j = 0; j < UPASS; ++j) {
+    const int64_t row = min(b0 + r0 + 16 * j, B - 1);      // (rows past the last repeat it and are not stored)
+    ub[j] = part_u + (row * NP * nhp + head) * d_u;
+    float m = -INFINITY, sum = 0.f, ms[NP];
+#pragma unroll
+    for (int s = 0; s < NP; ++s) {
+      scale[j][s] = part_l[(row * NP + s) * nhp + head];
+      ms[s] = part_m[(row * NP + s) * nhp + head];
+    }
+#pragma unroll
+    for (int s = 0; s < NP; ++s) m = scale[j][s] > 0.f ? fmaxf(m, ms[s]) : m;   // (an empty split has l = 0)
+#pragma unroll
+    for (int s = 0; s < NP; ++s) {
+      const float w = scale[j][s] > 0.f ? exp2f(ms[s] - m) : 0.f;
+      sum += w * scale[j][s];
+      scale[j][s] = w;
+    }
+    const float inv = sum > 0.f ? 1.f / sum : 0.f;
+#pragma unroll
+    for (int s = 0; s < NP; ++s) scale[j][s] *= inv;
+  }
+  auto load = [&](int k0) {
+#pragma unroll
+    for (int i = 0; i < WPASS; ++i) {
+      const int e = i * kMrThreads + tid, k = e / CPR, c = e % CPR;
+      wld[i] = *reinterpret_cast<const uint4*>(W_uv + ((int64_t)min(k0 + k, d_u - 1) * n_h + head) * DH + c * 8);
+    }
+#pragma unroll
+    for (int j = 0; j < UPASS; ++j)
+#pragma unroll
+      for (int s = 0; s < NP; ++s) uld[j][s] = *reinterpret_cast<const uint4*>(ub[j] + (int64_t)s * nhp * d_u + min(k0 + cl * 8, d_u - 8));
+  };
+  load(0);
+  mm_f32x16 acc[NT];
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) acc[nt] = (mm_f32x16)(0.f);
+  // wave <-> 32 rows and half of the head's outputs
+  const char* arow = ust + ((wave & 1) * 32 + n32) * kMrURow + hi * 16;
+  const int nt0 = (wave >> 1) * NT;
+  const int tr0 = (8 * (q16 >> 1) + (i16 >> 2)) * WROW + nt0 * 64 + 32 * (q16 & 1) + 8 * (i16 & 3);
+  for (int k0 = 0; k0 < d_u; k0 += kMmCols) {
+#pragma unroll
+    for (int j = 0; j < UPASS; ++j) {
+      float f[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+      if (k0 + cl * 8 < d_u) {                             // (a last stage of 64 columns: zeros against what repeats the last one)
+#pragma unroll
+        for (int s = 0; s < NP; ++s) {
+          const uint32_t uu[4] = {uld[j][s].x, uld[j][s].y, uld[j][s].z, uld[j][s].w};
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            f[2 * i] = fmaf(scale[j][s], __uint_as_float(uu[i] << 16), f[2 * i]);
+            f[2 * i + 1] = fmaf(scale[j][s], __uint_as_float(uu[i] & 0xffff0000u), f[2 * i + 1]);
+          }
+        }
+      }
+      mm_bf16x8 high, rest;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        high[i] = (__bf16)f[i];
+        rest[i] = (__bf16)(f[i] - (float)high[i]);
+      }
+      char* u = ust + (r0 + 16 * j) * kMrURow + cl * 16;
+      *reinterpret_cast<mm_bf16x8*>(u) = high;
+      *reinterpret_cast<mm_bf16x8*>(u + kMrRows * kMrURow) = rest;
+    }
+#pragma unroll
+    for (int i = 0; i < WPASS; ++i) {
+      const int e = i * kMrThreads + tid, k = e / CPR, c = e % CPR;
+      *reinterpret_cast<uint4*>(wst + k * WROW + c * 16) = wld[i];
+    }
+    __syncthreads();
+    if (k0 + kMmCols < d_u) load(k0 + kMmCols);
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+      const mm_bf16x8 a_hi = *reinterpret_cast<const mm_bf16x8*>(arow + ks * 32);
+      const mm_bf16x8 a_lo = *reinterpret_cast<const mm_bf16x8*>(arow + kMrRows * kMrURow + ks * 32);
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        const char* base = wst + tr0 + nt * 64 + ks * 16 * WROW;
+        const mm_s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((mm_lds_s16x4_t*)(base));
+        const mm_s16x4 hi4 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((mm_lds_s16x4_t*)(base + 4 * WROW));
+        const mm_bf16x8 w = __builtin_bit_cast(mm_bf16x8, __builtin_shufflevector(lo, hi4, 0, 1, 2, 3, 4, 5, 6, 7));
+        acc[nt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a_hi, w, acc[nt], 0, 0, 0);
+        acc[nt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a_lo, w, acc[nt], 0, 0, 0);
+      }
+    }
+    __syncthreads();
+  }
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt)                          // this lane: column (nt0 + nt) * 32 + n32, rows 8 g4 + 4 hi + {0..3}
+#pragma unroll
+    for (int g4 = 0; g4 < 4; ++g4)
+#pragma unroll
+      for (int v = 0; v < 4; ++v) {
+        const int b = b0 + (wave & 1) * 32 + 8 * g4 + 4 * hi + v;
+        if (b < B) st(out, ((int64_t)b * n_h + head) * DH + (nt0 + nt) * 32 + n32, acc[nt][4 * g4 + v]);
+      }
+}
+
 // Two rows and more, and a single one whose width the one-row merge does not take.
 bool merge_mfma_supported(const elitekv_dims& d, int d_u, int64_t B) {
   return (B >= 2 || merge_up_width(d.n_heads, d_u) == 0) && d_u % 64 == 0 && (d.head_dim == 128 || d.head_dim == 64);
@@ -291,6 +418,33 @@ static hipError_t launch_merge_mfma_dh(const DecodeArgs& a, const DecodePlan& p,
       (const bf16_t*)a.W_uv, (float*)(a.ws + p.off_opart), (int)a.B, d.n_heads, p.head_groups * 32, p.d_u,
       p.n_part, rows);
   return hipGetLastError();
+}
+
+bool merge_rows_pays(const DecodeArgs& a, const DecodePlan& p) {
+  return a.mapped && p.merge_batch && p.n_part <= kMrSplits && (a.B + kMrRows - 1) / kMrRows * a.dims.n_heads >= 256;
+}
+
+template <int DH, int NP>
+static hipError_t launch_merge_rows_as(const DecodeArgs& a, const DecodePlan& p, hipStream_t stream) {
+  const elitekv_dims& d = a.dims;
+  constexpr size_t lds = (size_t)MergeMfmaLayout<DH>::WST + (size_t)2 * kMrRows * kMrURow;
+  static LdsLimit limit;
+  const hipError_t e = raise_lds_limit(limit, reinterpret_cast<const void*>(&merge_rows_kernel<DH, NP>), lds);
+  if (e != hipSuccess) return e;
+  merge_rows_kernel<DH, NP><<<dim3(d.n_heads, (unsigned)((a.B + kMrRows - 1) / kMrRows)), kMrThreads, lds, stream>>>(
+      (const float*)(a.ws + p.off_m), (const float*)(a.ws + p.off_l), (const bf16_t*)(a.ws + p.off_u), (const bf16_t*)a.W_uv,
+      (bf16_t*)a.out, (int)a.B, d.n_heads, p.head_groups * 32, p.d_u);
+  return hipGetLastError();
+}
+template <int DH>
+static hipError_t launch_merge_rows_dh(const DecodeArgs& a, const DecodePlan& p, hipStream_t stream) {
+  return p.n_part == 1   ? launch_merge_rows_as<DH, 1>(a, p, stream)
+         : p.n_part == 2 ? launch_merge_rows_as<DH, 2>(a, p, stream)
+         : p.n_part == 3 ? launch_merge_rows_as<DH, 3>(a, p, stream)
+                         : launch_merge_rows_as<DH, 4>(a, p, stream);
+}
+hipError_t launch_merge_rows(const DecodeArgs& a, const DecodePlan& p, hipStream_t stream) {
+  return a.dims.head_dim == 128 ? launch_merge_rows_dh<128>(a, p, stream) : launch_merge_rows_dh<64>(a, p, stream);
 }
 
 hipError_t launch_merge_mfma(const DecodeArgs& a, const DecodePlan& p, hipStream_t stream) {

@@ -242,9 +242,9 @@ hipError_t launch_tree_plan(const int32_t* parent, const int32_t* prefix_len, co
 // ---- the accepted path ----
 // Row prefix + k takes what row prefix + path[k] holds, k <= path[k], for both planes; a rotated key stays as it is: a node's
 // position is prefix + its depth, and the k-th node of a path has depth k.  A thread owns a piece of the row for every k, so no
-// two threads touch the same bytes: rows that are sources of later copies lie at or behind the rows written so far, and eight
+// two threads touch the same bytes: rows that are sources of later copies lie at or behind the rows written so far, and 32
 // copies are loaded ahead of the first of them being stored.
-constexpr int kCommitAhead = 8;
+constexpr int kCommitAhead = 32;
 
 template <typename U>
 __global__ __launch_bounds__(256) void tree_commit_kernel(const int32_t* __restrict__ path, const int32_t* __restrict__ path_len,

@@ -28,9 +28,10 @@ inline size_t qprep_mfma_lds(int head_dim, int r) { return (size_t)kQmRows * (he
 
 // bx = block of 128 latent columns, by = head; qms = qprep_mfma_lds(...) bytes of 16-byte aligned LDS;
 // KS = contraction steps of 16 non-elite dims (the tail is zero-filled).  P.sincos (optional) is written by the
-// work-groups that rotate the elite query.
-template <int KS>
-__device__ __forceinline__ void qprep_mfma_body(const QprepRowsParams& P, const RopeTable& rope, int bx, int by,
+// work-groups that rotate the elite query.  Rows b_lo .. b_hi - 1.
+// MANY: a launch of many rows; the rows of a pass are requested all at once (one after the other, a pass waits for memory sixteen times).
+template <int KS, bool MANY = false>
+__device__ __forceinline__ void qprep_mfma_body(const QprepRowsParams& P, const RopeTable& rope, int bx, int by, int b_lo, int b_hi,
                                                 char* qms) {
   const bf16_t* __restrict__ q = P.q;
   const int32_t* __restrict__ q_pos = P.q_pos;
@@ -38,7 +39,7 @@ __device__ __forceinline__ void qprep_mfma_body(const QprepRowsParams& P, const 
   const int32_t* __restrict__ elite_idx = P.elite_idx;
   float* __restrict__ qe = P.qe;
   bf16_t* __restrict__ qt = P.qt;
-  const int B = P.B, n_h = P.n_h, d_h = P.d_h, r = P.r, d_c = P.d_c;
+  const int B = b_hi, n_h = P.n_h, d_h = P.d_h, r = P.r, d_c = P.d_c;
   const float scale_log2e = P.scale_log2e;
   const int nd = d_h - 2 * r, half = d_h / 2, ndp = nd + 8;
   uint16_t* qne = reinterpret_cast<uint16_t*>(qms);                       // [kQmRows][ndp] bf16 bits
@@ -73,14 +74,25 @@ __device__ __forceinline__ void qprep_mfma_body(const QprepRowsParams& P, const 
   const uint32_t* q32 = reinterpret_cast<const uint32_t*>(q);
   const int my_chunk = (lane < nd / 2) ? ne[lane] : 0;
 
-  for (int b0 = 0; b0 < B; b0 += kQmRows) {
+  for (int b0 = b_lo; b0 < B; b0 += kQmRows) {
     const int rows = min(kQmRows, B - b0);
-    if (b0 > 0) __syncthreads();                        // the previous rows have been consumed
+    if (b0 > b_lo) __syncthreads();                      // the previous rows have been consumed
     // compacted non-elite query: lane <-> chunk position, wave <-> rows wave, wave + 4, ...
-    for (int bl = wave; bl < kQmRows; bl += 4) {
-      uint32_t* dst = reinterpret_cast<uint32_t*>(qne + bl * ndp);
-      if (lane < nd / 2) dst[lane] = (bl < rows) ? q32[((int64_t)(b0 + bl) * n_h + h) * half + my_chunk] : 0u;
-      else if (lane < nd / 2 + 4) dst[lane] = 0u;       // the padding doubles as the zero tail of K
+    if constexpr (MANY) {
+      uint32_t v[kQmRows / 4];
+#pragma unroll
+      for (int i = 0; i < kQmRows / 4; ++i) v[i] = q32[((int64_t)min(b0 + wave + 4 * i, B - 1) * n_h + h) * half + my_chunk];
+#pragma unroll
+      for (int i = 0; i < kQmRows / 4; ++i) {
+        const int bl = wave + 4 * i;
+        if (lane < nd / 2 + 4) reinterpret_cast<uint32_t*>(qne + bl * ndp)[lane] = bl < rows && lane < nd / 2 ? v[i] : 0u;
+      }
+    } else {
+      for (int bl = wave; bl < kQmRows; bl += 4) {
+        uint32_t* dst = reinterpret_cast<uint32_t*>(qne + bl * ndp);
+        if (lane < nd / 2) dst[lane] = (bl < rows) ? q32[((int64_t)(b0 + bl) * n_h + h) * half + my_chunk] : 0u;
+        else if (lane < nd / 2 + 4) dst[lane] = 0u;     // the padding doubles as the zero tail of K
+      }
     }
     if (bx == 0) {                              // rotated elite query of these rows
       for (int e = tid; e < rows * r; e += 256) {
