@@ -476,11 +476,11 @@ def elitekv_page_plan(cached_len, new_len, page_rows, n_pages, block_table, held
     """cached_len, new_len, held, held_out [B] int32; block_table [B, cols] int32; free_pages [n_pages] int32;
     free_span, free_span_out [2] int64; pos, kv_len [B, T] int32, slot [B, T] int64."""
     B, T = pos.shape
-    ws_bytes = 0 if ws is None else ws.numel() * ws.element_size()
-    st = _lib.elitekv_page_plan(_ptr(cached_len), _ptr(new_len), B, T, int(page_rows), int(n_pages), _ptr(block_table),
-                                _cols(block_table), _ptr(held), _ptr(held_out), _ptr(free_pages), _ptr(free_span),
-                                _ptr(free_span_out), _ptr(pos), _ptr(slot), _ptr(kv_len), _ptr(ws), ws_bytes,
-                                _stream(stream))
+    ws_bytes = 0 if ws is None else ws.nbytes
+    st = _lib.elitekv_page_plan(cached_len.data_ptr(), new_len.data_ptr(), B, T, page_rows, n_pages, block_table.data_ptr(),
+                                block_table.shape[1], held.data_ptr(), held_out.data_ptr(), free_pages.data_ptr(),
+                                free_span.data_ptr(), free_span_out.data_ptr(), pos.data_ptr(), slot.data_ptr(),
+                                kv_len.data_ptr(), _ptr(ws), ws_bytes, _stream(stream))
     _check(st, "elitekv_page_plan")
 
 
@@ -504,7 +504,8 @@ def elitekv_paged_attn(dims, q, q_pos, kv_len, max_seq_len, block_table, page_ro
 def elitekv_tree_plan(parent, prefix_len, n_nodes, pos, mask, stream=None):
     """parent, pos [B, T] int32; prefix_len, n_nodes [B] int32; mask [B, T, ceil(T / 32)] int32 (bits)."""
     B, T = parent.shape
-    st = _lib.elitekv_tree_plan(_ptr(parent), _ptr(prefix_len), _ptr(n_nodes), B, T, _ptr(pos), _ptr(mask), _stream(stream))
+    st = _lib.elitekv_tree_plan(parent.data_ptr(), prefix_len.data_ptr(), n_nodes.data_ptr(), B, T, pos.data_ptr(),
+                                mask.data_ptr(), _stream(stream))
     _check(st, "elitekv_tree_plan")
 
 

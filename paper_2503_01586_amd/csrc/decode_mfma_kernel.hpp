@@ -450,7 +450,7 @@ __global__ __launch_bounds__(NW * 64, (AttnMfmaLayout<NW, DC_W, TWO_R>::kGroupsP
   int64_t end_row = 0;
   if constexpr (MAPPED) {
     t_end = seen.len;
-    if (seen.len > 0) end_row = seen.row(seen.len - 1, seen.page(seen.len - 1));
+    if (seen.mask && seen.len > 0) end_row = seen.row(seen.len - 1, seen.page(seen.len - 1));   // (without a mask every tile has a row)
   }
 
   f32x16 uacc[CT];

@@ -117,7 +117,30 @@ __global__ __launch_bounds__(kPlanThreads) void page_plan_small_kernel(const Pag
   for (int e = tid; e < tokens; e += kPlanThreads) page_token(a, e / a.T, e % a.T, rec[e / a.T]);
 }
 
-// The others: the records first, then a wave for every request's pages and a thread for every token.
+// The others.  Up to 1024 requests whose counts are not updated in place: every work-group forms all records for itself and fills its
+// share.  Else the records first, then a wave for every request's pages and a thread for every token.
+constexpr int kFillTokens = 4096;            // tokens of a work-group
+__global__ __launch_bounds__(kPlanThreads) void page_plan_kernel(const PagePlanArgs a, int token_groups) {
+  __shared__ int64_t sums[2 * kPlanThreads / 64];
+  __shared__ PageRecord rec[kPlanThreads];
+  const int tid = threadIdx.x;
+  const int64_t taken = a.span[0], given = a.span[1];
+  int64_t grown = 0, back = 0;
+  page_records(a, 0, taken, given, grown, back, rec + tid, sums);
+  __syncthreads();
+  if ((int)blockIdx.x < token_groups) {
+    const int64_t end = min((int64_t)(blockIdx.x + 1) * kFillTokens, a.B * a.T);
+    for (int64_t e = (int64_t)blockIdx.x * kFillTokens + tid; e < end; e += kPlanThreads) {
+      const int b = (int)(e / a.T);
+      page_token(a, b, (int)(e - (int64_t)b * a.T), rec[b]);
+    }
+  } else {
+    const int g = blockIdx.x - token_groups, b = g * (kPlanThreads / 64) + (tid >> 6);
+    if (b < a.B) page_moves(a, b, rec[b], tid & 63, 64);
+    if (g == 0 && tid == 0) page_totals(a, taken, given, grown, back);
+  }
+}
+
 __global__ __launch_bounds__(kPlanThreads) void page_records_kernel(const PagePlanArgs a) {
   __shared__ int64_t sums[2 * kPlanThreads / 64];
   const int64_t taken = a.span[0], given = a.span[1];
@@ -146,6 +169,11 @@ size_t page_plan_workspace(int64_t B) { return (size_t)B * sizeof(PageRecord); }
 hipError_t launch_page_plan(const PagePlanArgs& a, hipStream_t stream) {
   if (a.B <= kPlanThreads && a.B * a.T <= 4 * kPlanThreads) {
     page_plan_small_kernel<<<1, kPlanThreads, 0, stream>>>(a);
+    return hipGetLastError();
+  }
+  if (a.B <= kPlanThreads && a.held_out != a.held && a.span_out != a.span) {
+    const int64_t groups = (a.B * a.T + kFillTokens - 1) / kFillTokens;
+    page_plan_kernel<<<(unsigned)(groups + (a.B + kPlanThreads / 64 - 1) / (kPlanThreads / 64)), kPlanThreads, 0, stream>>>(a, (int)groups);
     return hipGetLastError();
   }
   page_records_kernel<<<1, kPlanThreads, 0, stream>>>(a);
@@ -242,9 +270,9 @@ hipError_t launch_tree_plan(const int32_t* parent, const int32_t* prefix_len, co
 // ---- the accepted path ----
 // Row prefix + k takes what row prefix + path[k] holds, k <= path[k], for both planes; a rotated key stays as it is: a node's
 // position is prefix + its depth, and the k-th node of a path has depth k.  A thread owns a piece of the row for every k, so no
-// two threads touch the same bytes: rows that are sources of later copies lie at or behind the rows written so far, and 32
+// two threads touch the same bytes: rows that are sources of later copies lie at or behind the rows written so far, and 16
 // copies are loaded ahead of the first of them being stored.
-constexpr int kCommitAhead = 32;
+constexpr int kCommitAhead = 16;
 
 template <typename U>
 __global__ __launch_bounds__(256) void tree_commit_kernel(const int32_t* __restrict__ path, const int32_t* __restrict__ path_len,
@@ -252,13 +280,14 @@ __global__ __launch_bounds__(256) void tree_commit_kernel(const int32_t* __restr
                                                           int64_t plane_rows, int64_t cap, const RowMap map, U* ke_plane, U* c_plane, int ke_units,
                                                           int c_units) {
   __shared__ int64_t from[kTreeNodes], to[kTreeNodes];
-  const int tid = threadIdx.x;
+  __shared__ int first[2];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int64_t b = blockIdx.y;
   const int n = min(path_len[b], T);
   const int64_t prefix = prefix_len[b];
+  int64_t f = -1, t = -1;
   if (tid < n) {
     const int node = path[b * T + tid];
-    int64_t f = -1, t = -1;
     if (prefix >= 0 && node > tid && node < T && prefix + node < cap) {
       auto row = [&](int64_t j) -> int64_t {
         if (!map.table) return b * stride + j < plane_rows ? b * stride + j : -1;
@@ -267,24 +296,31 @@ __global__ __launch_bounds__(256) void tree_commit_kernel(const int32_t* __restr
       };
       f = row(prefix + node);
       t = row(prefix + tid);
-      if (f < 0 || t < 0) f = t = -1;
     }
-    from[tid] = f;
-    to[tid] = t;
   }
+  // the copies there are, in their order
+  const bool real = f >= 0 && t >= 0;
+  const uint64_t all = __ballot(real);
+  if (lane == 0 && wave < 2) first[wave] = __popcll(all);
+  __syncthreads();
+  if (real) {
+    const int at = __popcll(all & ((1ull << lane) - 1ull)) + (wave > 0 ? first[0] : 0);
+    from[at] = f;
+    to[at] = t;
+  }
+  const int m = __builtin_amdgcn_readfirstlane(first[0] + first[1]);
   __syncthreads();
   const int u = blockIdx.x * 256 + tid;
-  if (u >= ke_units + c_units) return;
+  if (m == 0 || u >= ke_units + c_units) return;
   U* plane = u < ke_units ? ke_plane + u : c_plane + (u - ke_units);
   const int64_t row_units = u < ke_units ? ke_units : c_units;
-  for (int k0 = 0; k0 < n; k0 += kCommitAhead) {
+  for (int k0 = 0; k0 < m; k0 += kCommitAhead) {
     U v[kCommitAhead];
 #pragma unroll
-    for (int i = 0; i < kCommitAhead; ++i)
-      if (k0 + i < n && from[k0 + i] >= 0) v[i] = plane[from[k0 + i] * row_units];
+    for (int i = 0; i < kCommitAhead; ++i) v[i] = plane[from[min(k0 + i, m - 1)] * row_units];   // (past the last: the last again)
 #pragma unroll
     for (int i = 0; i < kCommitAhead; ++i)
-      if (k0 + i < n && to[k0 + i] >= 0) plane[to[k0 + i] * row_units] = v[i];
+      if (k0 + i < m) plane[to[k0 + i] * row_units] = v[i];
   }
 }
 
