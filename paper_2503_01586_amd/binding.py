@@ -464,7 +464,11 @@ TREE_MAX_NODES = 128   # ELITEKV_TREE_MAX_NODES
 
 
 def _cols(block_table):
-    return 0 if block_table is None else int(block_table.shape[1])
+    if block_table is None:
+        return 0
+    if not block_table.is_contiguous():                    # (a table's columns are its row stride)
+        raise ValueError("block_table: its rows have to lie back to back")
+    return block_table.shape[1]
 
 
 def elitekv_page_plan_workspace_bytes(B, T) -> int:
@@ -478,7 +482,7 @@ def elitekv_page_plan(cached_len, new_len, page_rows, n_pages, block_table, held
     B, T = pos.shape
     ws_bytes = 0 if ws is None else ws.nbytes
     st = _lib.elitekv_page_plan(cached_len.data_ptr(), new_len.data_ptr(), B, T, page_rows, n_pages, block_table.data_ptr(),
-                                block_table.shape[1], held.data_ptr(), held_out.data_ptr(), free_pages.data_ptr(),
+                                _cols(block_table), held.data_ptr(), held_out.data_ptr(), free_pages.data_ptr(),
                                 free_span.data_ptr(), free_span_out.data_ptr(), pos.data_ptr(), slot.data_ptr(),
                                 kv_len.data_ptr(), _ptr(ws), ws_bytes, _stream(stream))
     _check(st, "elitekv_page_plan")

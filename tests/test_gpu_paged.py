@@ -3,7 +3,9 @@
 Bounds.  fp32: the parity gate of the decode kernels, max-abs-rel 1e-5.  bf16: their 2e-2, and as a 2-norm 5e-3: the absorbed query,
 the probabilities, the splits' accumulators and the result are each rounded to bf16 once, a step of 2^-8 relative at most, uniform, so
 2^-8 / sqrt(3) x 0.72 (mean of the mantissa's square) = 1.6e-3 in the 2-norm each, the query's twice (through the scores of two sums):
-sqrt(5) x 1.6e-3 = 3.6e-3.  A tile lost or seen twice among the few hundred rows here is more than 5e-2.
+sqrt(5) x 1.6e-3 = 3.6e-3, with a third as much again for what depends on the draw: 5e-3.  A query g times as large has scores, and so
+errors of its own rounding in them (absolute ones, which are the probabilities' relative ones), g times as large: sqrt(3 + 2 g^2) x
+1.6e-3 and the third, for g = 4 1.3e-2.  A tile lost or seen twice among the few hundred rows here is more than 5e-2.
 Plans, masks and moved rows are whole numbers and copies: equal."""
 import numpy as np
 import pytest
@@ -35,14 +37,14 @@ SHAPES = {
 }
 
 
-def _close(name, got, ref, dtype):
+def _close(name, got, ref, dtype, g=1):
     assert np.all(np.isfinite(got)), name
     err = orc.max_abs_rel(got, ref)
     norm = np.linalg.norm(got - ref) / max(np.linalg.norm(ref), 1e-30)
     print("%-40s max-abs-rel %.2e  2-norm %.2e" % (name, err, norm), flush=True)
     assert err <= TOL[dtype], name
     if dtype == "bf16":
-        assert norm <= 5e-3, name
+        assert norm <= {1: 5e-3, 4: 1.3e-2}[g], name
 
 
 class Cache:
@@ -166,6 +168,104 @@ def test_lengths_past_the_table_and_the_bound_are_cut(name):
     assert np.all(got[1] == 0.0)
 
 
+@pytest.mark.parametrize("name", ["7b", "13b", "12pct", "r16_72_heads", "slrd", "fp32_tiled", "fp32_any"])
+def test_long_caches_and_peaked_scores(name):
+    """Many tiles per work-group and a query four times as large: maxima rise in many tiles, and a tile lost or read twice shows.  One
+    request alone as well."""
+    print("long caches", name, flush=True)
+    for lens, splits in (([3001, 1777], (0, 1, 7)), ([2500], (0, 1))):
+        k = Cache(name, lens, 64, seed=51)
+        q = k.queries(1) * 4
+        pos = np.array([[n - 1] for n in lens])
+        ref = k.reference(q, pos, [np.ones((1, n), dtype=bool) for n in lens])
+        for ns in splits:
+            _close("%s %s splits %d" % (name, lens, ns), host64(k.paged(q, pos, pos + 1, ns)), ref, k.dt, g=4)
+
+
+@pytest.mark.parametrize("name", ["7b", "13b", "slrd", "fp32_tiled"])
+def test_trees_over_long_caches(name):
+    print("trees over long caches", name, flush=True)
+    prefix, nodes, T = np.array([1990, 700]), np.array([9, 7]), 9
+    lens = [int(p + n) for p, n in zip(prefix, nodes)]
+    k = Cache(name, lens, 32, seed=52)
+    q = k.queries(T) * 4
+    sees = np.stack([orc.tree_sees(_random_tree(k.rng, T), n) for n in nodes])
+    pos = prefix[:, None] + np.maximum(sees.sum(axis=2) - 1, 0)
+    seen = []
+    for b, n in enumerate(lens):
+        s = np.zeros((T, n), dtype=bool)
+        s[:nodes[b], :prefix[b]] = True
+        s[:, prefix[b]:] = sees[b][:, :nodes[b]]
+        seen.append(s)
+    ref = k.reference(q, pos, seen)
+    for ns in (0, 1, 5):
+        _close("%s splits %d" % (name, ns), host64(k.tree(q, pos, prefix, nodes, sees, ns)), ref, k.dt, g=4)
+
+
+@pytest.mark.parametrize("name,planes_gb", [("12pct", 5.0), ("fp32_tiled", 5.0), ("fp32_any", 5.0)])
+def test_pages_beyond_four_gigabytes(name, planes_gb):
+    """Planes of which both are larger than 2^32 bytes, the cached rows in their last pages; attention, and a commit among them."""
+    print("beyond 4 GiB", name, flush=True)
+    sh, _ = SHAPES[name]
+    dt = torch.bfloat16 if sh["dtype"] == "bf16" else torch.float32
+    e, page = dt.itemsize, 16
+    rows = int(planes_gb * 2**30 / (min(2 * sh["r"] * sh["n_heads"], sh["d_c"]) * e)) // page * page
+    lens = [40, 21]
+    k = Cache(name, lens, page, seed=53)
+    small_ke, small_c, old = k.ke, k.c, [r.copy() for r in k.rows]
+    k.ke = torch.empty(rows, sh["n_heads"], 2 * sh["r"], dtype=dt, device=DEV)
+    k.c = torch.empty(rows, sh["d_c"], dtype=dt, device=DEV)
+    assert k.ke.numel() * e > 2**32 and k.c.numel() * e > 2**32
+    shift = rows // page - k.n_pages
+    need = [-(-n // page) for n in lens]
+    for b, n in enumerate(need):
+        k.table[b, :n] += shift
+    k.rows = [r + shift * page for r in k.rows]
+    for b in range(2):
+        k.ke[torch.from_numpy(k.rows[b]).to(DEV)] = small_ke[torch.from_numpy(old[b]).to(DEV)]
+        k.c[torch.from_numpy(k.rows[b]).to(DEV)] = small_c[torch.from_numpy(old[b]).to(DEV)]
+    q, pos = k.queries(1), np.array([[n - 1] for n in lens])
+    got = host64(k.paged(q, pos, pos + 1))
+    big_ke, big_c, big_rows, k.ke, k.c, k.rows = k.ke, k.c, k.rows, small_ke, small_c, old
+    _close(name, got, k.reference(q, pos, [np.ones((1, n), dtype=bool) for n in lens]), k.dt)
+    path = np.zeros((2, 10), dtype=int)                    # (trees of ten nodes: an entry is a node below ten)
+    path[0, :3], path[1, :2] = [3, 5, 9], [1, 2]
+    ekv.elitekv_tree_commit(k.dims, i32(path), i32([3, 2]), i32([30, 17]), 0, big_ke, big_c, block_table=i32(k.table), page_rows=page)
+    torch.cuda.synchronize()
+    for b, (P, n) in enumerate([(30, 3), (17, 2)]):
+        for i in range(n):
+            to, of = int(big_rows[b][P + i]), int(old[b][P + path[b, i]])
+            assert torch.equal(big_c[to], small_c[of]) and torch.equal(big_ke[to], small_ke[of])
+    del big_ke, big_c
+    torch.cuda.empty_cache()
+
+
+def test_a_call_on_another_stream_and_pages_of_many_rows():
+    lens = [1000, 77]
+    k = Cache("7b", lens, 1024, seed=54)
+    q, pos = k.queries(1), np.array([[n - 1] for n in lens])
+    ref = k.reference(q, pos, [np.ones((1, n), dtype=bool) for n in lens])
+    side = torch.cuda.Stream()
+    out = k.blank(q)
+    torch.cuda.synchronize()
+    _close("by argument", host64(k.paged(q, pos, pos + 1, stream=side, out=out)), ref, k.dt)
+    with torch.cuda.stream(side):
+        _close("current", host64(k.paged(q, pos, pos + 1)), ref, k.dt)
+
+
+def test_nothing_to_see():
+    """A bound of zero rows, planes without a whole page, an empty batch."""
+    k = Cache("7b", [40, 30], 64, seed=55)
+    q, pos = k.queries(2), np.array([[38, 39], [28, 29]])
+    assert torch.all(k.paged(q, pos, pos + 1, max_seq=0) == 0)
+    out = k.blank(q)
+    ws = torch.empty(ekv.elitekv_paged_attn_workspace_bytes(k.dims, 2, 2, 40), dtype=torch.uint8, device=DEV)
+    ekv.elitekv_paged_attn(k.dims, q, i32(pos), i32(pos + 1), 40, i32(k.table), 64, k.W_uk, k.W_uv, i32(k.idx), k.ke, k.c, out, ws, plane_rows=63)
+    torch.cuda.synchronize()
+    assert torch.all(out == 0)
+    ekv.elitekv_paged_attn(k.dims, q[:0], i32(pos[:0]), i32(pos[:0]), 40, i32(k.table[:0]), 64, k.W_uk, k.W_uv, i32(k.idx), k.ke, k.c, out, ws)
+
+
 PROMPTS = {
     "7b": (shape(64, 32, 128, 8, 1536, "bf16"), 0),
     "r4": (shape(64, 16, 128, 4, 256, "bf16"), 0),
@@ -280,6 +380,39 @@ def test_any_mask_and_rows_that_nobody_sees(name, T):
         _close("%s T %d splits %d" % (name, T, ns), got, ref, k.dt)
         for b in range(3):
             assert np.all(got[b][~seen[b].any(axis=1)] == 0.0)
+
+
+MANY = {
+    "72_heads": (shape(64, 72, 128, 16, 256, "bf16"), 0),
+    "head_64": (shape(64, 72, 64, 4, 128, "bf16"), 0),
+    "slrd_320": (shape(64, 64, 128, 4, 640, "bf16"), 320),
+}
+
+
+@pytest.mark.parametrize("name", list(MANY))
+def test_many_rows(name, monkeypatch):
+    """Enough rows and heads for the merge that keeps its sum in the accumulators, with one to four splits, a last stage of 64 latent
+    columns and rows past the last; five splits take the other one."""
+    print("many rows", name, flush=True)
+    monkeypatch.setitem(SHAPES, name, MANY[name])
+    T, prefix = 100, np.array([60, 0, 33])
+    nodes = np.array([100, 97, 100])
+    lens = [int(p + n) for p, n in zip(prefix, nodes)]
+    k = Cache(name, lens, 16, seed=61)
+    q = k.queries(T)
+    sees = np.stack([orc.tree_sees(_random_tree(k.rng, T), n) for n in nodes])
+    pos = prefix[:, None] + np.maximum(sees.sum(axis=2) - 1, 0)
+    seen = []
+    for b, n in enumerate(lens):
+        s = np.zeros((T, n), dtype=bool)
+        s[:nodes[b], :prefix[b]] = True
+        s[:, prefix[b]:] = sees[b][:, :nodes[b]]
+        seen.append(s)
+    ref = k.reference(q, pos, seen)
+    for ns in (1, 2, 3, 4, 5):
+        got = host64(k.tree(q, pos, prefix, nodes, sees, ns))
+        _close("%s splits %d" % (name, ns), got, ref, k.dt)
+        assert np.all(got[1, 97:] == 0.0)
 
 
 @pytest.mark.parametrize("name", ["7b", "fp32_tiled", "fp32_any"])

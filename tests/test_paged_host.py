@@ -67,6 +67,16 @@ def test_paged_attn_refusals(shape):
     assert ekv.elitekv_paged_attn_workspace_bytes(d, 300, 300, 60) == 0
 
 
+def test_a_table_with_gaps_between_its_rows_is_refused():
+    import torch
+    d, t = _dims(), torch.zeros(2, 8, dtype=torch.int32)
+    q, planes = torch.zeros(2, 1, 4, 32), torch.zeros(64, 64)
+    with pytest.raises(ValueError):
+        ekv.elitekv_paged_attn(d, q, t, t, 16, t[:, :4], 16, q, q, t, planes, planes, q, None, stream=0)
+    with pytest.raises(ValueError):
+        ekv.elitekv_tree_commit(d, t, t, t, 0, planes, planes, block_table=t[:, ::2], page_rows=16, stream=0)
+
+
 def test_prompt_workspaces():
     """Many queries: room for the gathered rows and what the prefill's kernels need; a size serves every shorter bound."""
     d = ekv.make_dims(64, 32, 128, 8, 1536, "bf16")
