@@ -6,21 +6,9 @@
 // The path of the remaining shapes (decode_generic.hip, append_generic.hip) gives a work-group one head or 256 columns
 // and walks the whole contraction serially: 64 work-groups on 256 compute units, one load in flight per lane.
 // Measured at 7B 25 %, fp32, two sequences of 1000 tokens (us): append 554, query 44, attention 190, merge 291.
-#include "common.hpp"
-#include "launch.hpp"
+#include "tiled_f32.hpp"
 
 namespace ekv {
-
-typedef __attribute__((ext_vector_type(4))) float tf_f32x4;
-
-__device__ __forceinline__ tf_f32x4 ld4(const float* p) { return *reinterpret_cast<const tf_f32x4*>(p); }
-__device__ __forceinline__ tf_f32x4 ld4(const bf16_t* p) {
-  const uint2 v = *reinterpret_cast<const uint2*>(p);
-  tf_f32x4 r;
-  r[0] = __uint_as_float(v.x << 16); r[1] = __uint_as_float(v.x & 0xffff0000u);
-  r[2] = __uint_as_float(v.y << 16); r[3] = __uint_as_float(v.y & 0xffff0000u);
-  return r;
-}
 
 // ---- append: Y = X [W_ke | W_dkv | W_dkv2], rotated and stored ----
 // A work-group owns 16 columns and the whole contraction for TT tokens: 256 groups of four lanes, a group takes every
@@ -278,16 +266,12 @@ __global__ __launch_bounds__(kTaThreads) void front_tiled_kernel(
 // whose keys differ from head to head, is added by vector instructions, two tokens per wave.  Bound by the fp32 matrix
 // cores (d_c / 2 instructions of 32 cycles per tile and 16 heads) and, at a few tiles per work-group, by the start.
 // Two sequences of 1000 tokens, 7B 25 %: 18 us (attn_generic_kernel 190).
-// MAPPED: rows in pages or behind a tree's mask (a tile of 16 rows lies inside one page); a latent row that is not seen counts as
-// zeros, whatever it holds.
-constexpr int kTtTok = 16, kTtWaves = 8, kTtKeRegs = 4, kTtComputeUnits = 256;
-
-template <typename T, int CPW, bool MAPPED>
+template <typename T, int CPW>
 __global__ __launch_bounds__(kTtWaves * 64) void attn_tiled_kernel(
     const T* __restrict__ ke_plane, const T* __restrict__ c_plane, const float* __restrict__ qe,
     const float* __restrict__ qt, const int32_t* __restrict__ seq_len, float* __restrict__ part_m,
     float* __restrict__ part_l, float* __restrict__ part_u, int n_h, int two_r, int d_c, int d_q, int d_u,
-    int64_t max_seq_len, int64_t batch_stride_rows, int64_t plane_rows, int n_splits, int q_per_seq, RowMap map) {
+    int64_t max_seq_len, int64_t batch_stride_rows, int64_t plane_rows, int n_splits, int q_per_seq) {
   constexpr int CS = CPW * 16 + 4;                        // row of a wave's slice in LDS: conflict-free both ways
   extern __shared__ __align__(16) float smem[];
   float* cs = smem + (threadIdx.x >> 6) * kTtTok * CS;    // [wave][16 tokens][CS]
@@ -301,19 +285,18 @@ __global__ __launch_bounds__(kTtWaves * 64) void attn_tiled_kernel(
   const int head_ld = min(head, n_h - 1);                 // lanes past the last head repeat it and store nothing
 
   const int64_t row0 = (int64_t)(b / q_per_seq) * batch_stride_rows;
-  const int64_t cap = map.table ? max_seq_len : min(max_seq_len, plane_rows - row0);
-  const SeenRows seen(map, seq_len, b, q_per_seq, batch_stride_rows, cap);
-  const int64_t len = seen.len;
+  int64_t len = seq_len[b];
+  len = min(len, max_seq_len);
+  len = min(len, plane_rows - row0);
+  len = max(len, (int64_t)0);
   const int64_t n_tiles = (len + kTtTok - 1) / kTtTok;
 
   const int blk0 = wave * CPW, v_blk0 = (d_c - d_u) / 16, q_blks = d_q / 16, n_blks = d_c / 16;
   auto load_tile = [&](int64_t tile, tf_f32x4 (&cv)[CPW]) {
     const int64_t tok = min(tile * kTtTok + i16, len - 1);
-    const int64_t row = MAPPED ? seen.row(tile * kTtTok, seen.page(tile * kTtTok)) + (tok - tile * kTtTok) : row0 + tok;
-    const bool sees = !MAPPED || (seen.tile(tile * kTtTok) >> i16) & 1u;
-    const T* src = c_plane + row * d_c + blk0 * 16 + quad * 4;
+    const T* src = c_plane + (row0 + tok) * d_c + blk0 * 16 + quad * 4;
 #pragma unroll
-    for (int i = 0; i < CPW; ++i) cv[i] = blk0 + i < n_blks && sees ? ld4(src + i * 16) : (tf_f32x4)(0.f);
+    for (int i = 0; i < CPW; ++i) cv[i] = blk0 + i < n_blks ? ld4(src + i * 16) : (tf_f32x4)(0.f);
   };
 
   tf_f32x4 acc[CPW], cv[CPW], qv[CPW];
@@ -335,9 +318,7 @@ __global__ __launch_bounds__(kTtWaves * 64) void attn_tiled_kernel(
   const int ke_units = two_r / 4, ke_par = quad & 1, ke_tok = 2 * wave + (quad >> 1);
   int buf = 0;
   for (; tile < n_tiles; tile += n_splits, buf ^= 1) {
-    const int64_t ktok = min(tile * kTtTok + ke_tok, len - 1);
-    const T* krow = ke_plane + ((MAPPED ? seen.row(tile * kTtTok, seen.page(tile * kTtTok)) + (ktok - tile * kTtTok) : row0 + ktok) * n_h + head_ld) * two_r;
-    const uint32_t sees = MAPPED ? seen.tile(tile * kTtTok) : 0u;
+    const T* krow = ke_plane + ((row0 + min(tile * kTtTok + ke_tok, len - 1)) * n_h + head_ld) * two_r;
     tf_f32x4 kv[kTtKeRegs];
 #pragma unroll
     for (int u = 0; u < kTtKeRegs; ++u)
@@ -381,7 +362,7 @@ __global__ __launch_bounds__(kTtWaves * 64) void attn_tiled_kernel(
     for (int w = 0; w < kTtWaves; ++w) s += spb[w * 64 + lane];
 #pragma unroll
     for (int v = 0; v < 4; ++v)
-      if (MAPPED ? !((sees >> (quad * 4 + v)) & 1u) : tile * kTtTok + quad * 4 + v >= len) s[v] = -INFINITY;
+      if (tile * kTtTok + quad * 4 + v >= len) s[v] = -INFINITY;
     float mx = fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3]));
     mx = fmaxf(mx, __shfl_xor(mx, 16, kWave));
     mx = fmaxf(mx, __shfl_xor(mx, 32, kWave));
@@ -517,8 +498,6 @@ __global__ __launch_bounds__(256) void merge_tiled_kernel(const float* __restric
 // Work-group = (32 output columns of a head, up to BT query rows), the whole contraction: 128 groups of eight lanes, each
 // 128 bytes of every 128th row of W_uv, all of them in flight at once.  Bound by the bytes of W_uv.  
 // 25 MB in 9.2 us.
-constexpr int kTuCols = 32;
-
 template <typename T, int BT>
 __global__ __launch_bounds__(1024) void upproj_tiled_kernel(const float* __restrict__ ubar, int ubar_rows,
                                                             const T* __restrict__ W_uv, T* __restrict__ out, int B,
@@ -579,24 +558,18 @@ bool decode_tiled_supported(const elitekv_dims& d, int d_ck, int64_t rows, int64
          2 * d.r <= 128 && d.head_dim % kTuCols == 0 && d.head_dim <= 256;
 }
 
-template <typename T, int CPW, bool MAPPED>
-static hipError_t launch_attn_tiled_as(const DecodeArgs& a, const DecodePlan& p, const float* qe, const float* qt, float* pm,
+template <typename T, int CPW>
+static hipError_t launch_attn_tiled(const DecodeArgs& a, const DecodePlan& p, const float* qe, const float* qt, float* pm,
                                     float* pl, float* pu, hipStream_t stream) {
   static LdsLimit limit;
   const elitekv_dims& d = a.dims;
   const size_t lds = sizeof(float) * (size_t)(kTtWaves * kTtTok * (CPW * 16 + 4) + 2 * (kTtWaves + 1) * 256 + 32 * d.r);
-  const hipError_t e = raise_lds_limit(limit, (const void*)attn_tiled_kernel<T, CPW, MAPPED>, lds);
+  const hipError_t e = raise_lds_limit(limit, (const void*)attn_tiled_kernel<T, CPW>, lds);
   if (e != hipSuccess) return e;
-  attn_tiled_kernel<T, CPW, MAPPED><<<dim3(p.n_splits, (d.n_heads + 15) / 16, (unsigned)a.B), kTtWaves * 64, lds, stream>>>(
+  attn_tiled_kernel<T, CPW><<<dim3(p.n_splits, (d.n_heads + 15) / 16, (unsigned)a.B), kTtWaves * 64, lds, stream>>>(
       (const T*)a.ke_plane, (const T*)a.c_plane, qe, qt, a.seq_len, pm, pl, pu, d.n_heads, 2 * d.r, d.d_c, p.d_q, p.d_u,
-      a.max_seq_len, a.batch_stride_rows, a.plane_rows, p.n_splits, a.q_per_seq, a.map);
+      a.max_seq_len, a.batch_stride_rows, a.plane_rows, p.n_splits, a.q_per_seq);
   return hipGetLastError();
-}
-template <typename T, int CPW>
-static hipError_t launch_attn_tiled(const DecodeArgs& a, const DecodePlan& p, const float* qe, const float* qt, float* pm,
-                                    float* pl, float* pu, hipStream_t stream) {
-  return a.mapped ? launch_attn_tiled_as<T, CPW, true>(a, p, qe, qt, pm, pl, pu, stream)
-                  : launch_attn_tiled_as<T, CPW, false>(a, p, qe, qt, pm, pl, pu, stream);
 }
 
 template <typename T>
@@ -610,7 +583,11 @@ static hipError_t launch_decode_tiled_t(const DecodeArgs& a, const DecodePlan& p
   float* pu = (float*)(a.ws + p.off_u);
   float* ubar = (float*)(a.ws + p.off_opart);
   hipError_t e = hipSuccess;
-  if (a.stages & 1) {
+  const bool many = a.mapped && B >= kTsManyRows;
+  if ((a.stages & 1) && many) {
+    e = launch_qprep_many_tiled(a, p, qe, qt, stream);
+    if (e != hipSuccess) return e;
+  } else if (a.stages & 1) {
 #define EKV_QPREP(BT)                                                                                               \
   qprep_tiled_kernel<T, BT><<<dim3((p.d_q + 63) / 64, n_h, (B + BT - 1) / BT), 256, 0, stream>>>(      \
       (const T*)a.q, a.q_pos, (const T*)a.W_uk, a.elite_idx, qe, qt, B, n_h, d_h, d.r, p.d_q,                       \
@@ -620,7 +597,10 @@ static hipError_t launch_decode_tiled_t(const DecodeArgs& a, const DecodePlan& p
     else EKV_QPREP(4);
 #undef EKV_QPREP
   }
-  if (a.stages & 2) {
+  if ((a.stages & 2) && a.mapped) {
+    e = launch_attn_seen_tiled(a, p, qe, qt, pm, pl, pu, stream);
+    if (e != hipSuccess) return e;
+  } else if (a.stages & 2) {
     const int cpw = (d.d_c / 16 + kTtWaves - 1) / kTtWaves;
 #define EKV_ATTN(C) e = launch_attn_tiled<T, C>(a, p, qe, qt, pm, pl, pu, stream)
     if (cpw <= 2) EKV_ATTN(2);
@@ -637,6 +617,7 @@ static hipError_t launch_decode_tiled_t(const DecodeArgs& a, const DecodePlan& p
     const auto merge = (int64_t)grid.x * n_h * B <= kTmFewGroups ? merge_tiled_kernel<kTmAhead> : merge_tiled_kernel<0>;
     merge<<<grid, 256, sizeof(float) * (size_t)(1024 + 8 + p.n_splits), stream>>>(pm, pl, pu, ubar, p.ubar_rows, n_h, p.d_u,
                                                                                  p.n_splits);
+    if (many) return launch_upproj_many_tiled(a, p, ubar, stream);
 #define EKV_UP(BT)                                                                                              \
   {                                                                                                             \
     static LdsLimit limit;                                                                                      \

@@ -382,6 +382,46 @@ def test_any_mask_and_rows_that_nobody_sees(name, T):
             assert np.all(got[b][~seen[b].any(axis=1)] == 0.0)
 
 
+# the kernels in fp32 arithmetic: one block of latent columns a wave, a last wave whose window is moved back and waves without blocks, the
+# widest rows, elite keys that are not all requested ahead, separated latents whose boundary lies inside a wave's blocks
+F32 = {
+    "c16": (shape(64, 3, 64, 4, 16, "fp32"), 0),
+    "c144": (shape(64, 5, 64, 4, 144, "fp32"), 0),
+    "c576_r16": (shape(64, 17, 128, 16, 576, "fp32"), 0),
+    "c2048": (shape(64, 32, 128, 8, 2048, "fp32"), 0),
+    "c1536_r32": (shape(64, 18, 128, 32, 1536, "fp32"), 0),
+    "c256_r48_head_256": (shape(64, 4, 256, 48, 256, "fp32"), 0),
+    "slrd_48_of_208": (shape(64, 5, 64, 4, 208, "fp32"), 48),
+    "slrd_768_of_1536": (shape(64, 32, 128, 8, 1536, "fp32"), 768),
+    "bf16_c1040": (shape(64, 16, 128, 8, 1040, "bf16"), 0),
+}
+
+
+@pytest.mark.parametrize("T,page", [(2, 16), (11, 0), (37, 32)])
+@pytest.mark.parametrize("name", list(F32))
+def test_widths_in_fp32_arithmetic(name, T, page, monkeypatch):
+    print("fp32 arithmetic", name, T, page, flush=True)
+    monkeypatch.setitem(SHAPES, name, F32[name])
+    prefix = np.array([260, 0, 33])
+    nodes = np.array([T, T - 1, T])
+    lens = [int(p + n) for p, n in zip(prefix, nodes)]
+    k = Cache(name, lens, page, seed=71)
+    q = k.queries(T)
+    sees = np.stack([orc.tree_sees(_random_tree(k.rng, T), n) for n in nodes])
+    pos = prefix[:, None] + np.maximum(sees.sum(axis=2) - 1, 0)
+    seen = []
+    for b, n in enumerate(lens):
+        s = np.zeros((T, n), dtype=bool)
+        s[:nodes[b], :prefix[b]] = True
+        s[:, prefix[b]:] = sees[b][:, :nodes[b]]
+        seen.append(s)
+    ref = k.reference(q, pos, seen)
+    for ns in (0, 1, 3, 40):
+        got = host64(k.tree(q, pos, prefix, nodes, sees, ns))
+        _close("%s T %d page %d splits %d" % (name, T, page, ns), got, ref, k.dt)
+        assert np.all(got[1, T - 1:] == 0.0)
+
+
 MANY = {
     "72_heads": (shape(64, 72, 128, 16, 256, "bf16"), 0),
     "head_64": (shape(64, 72, 64, 4, 128, "bf16"), 0),
