@@ -500,8 +500,11 @@ int elitekv_page_plan(const int32_t* cached_len, const int32_t* new_len, int64_t
 /*
  * elitekv_multiquery_attn (T = 1: elitekv_decode_attn) over a cache in pages, and with d_ck > 0 their slrd_ forms (W_uk = B^k_S,
  * W_uv = B^v_S).  The arguments are theirs with the table in place of batch_stride_rows; kv_len is clamped to max_seq_len and to what
- * the table has room for.  Of every request only pages that hold one of the first kv_len rows are read; a table entry outside
- * [0, plane_rows / page_rows) counts as page 0.
+ * the table has room for.  A table entry outside [0, plane_rows / page_rows) counts as page 0; entries past a request's rows may hold
+ * anything, and what lies in rows that no query sees is not used.
+ * Many queries (where elitekv_prefill_attn rebuilds keys and values: bf16, T of 48 and more over more than 64 rows): the first
+ * min(max_seq_len, table_cols * page_rows) rows of every request are copied from their pages into ws, so a bound close to the longest
+ * length saves time and workspace; n_splits does not count there, and B * T may be up to 2^24.
  * Workspace and errors as elitekv_multiquery_attn; EINVAL also for page_rows and table_cols < 1, ENULL without a table.
  */
 size_t elitekv_paged_attn_workspace_bytes(const elitekv_dims* dims, int32_t d_ck, int64_t B, int64_t T, int64_t max_seq_len,

@@ -129,4 +129,12 @@ __device__ __forceinline__ void rope_sincos_poly(int32_t pos, double theta, floa
   *cs = (q == 0) ? c : (q == 1) ? -s : (q == 2) ? -c : s;
 }
 
+// the largest of the four lanes i16, i16 + 16, ... in each of them, without a trip through LDS
+__device__ __forceinline__ float max_of_quads(float x) {
+  const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  x = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+
 }  // namespace ekv

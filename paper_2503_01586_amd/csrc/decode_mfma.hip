@@ -101,7 +101,9 @@ hipError_t launch_decode_mfma(const DecodeArgs& a, const DecodePlan& p, hipStrea
   if (e != hipSuccess) return e;
   if (!(a.stages & 2)) return (a.stages & 4) ? launch_merge_up(a, p, stream) : hipSuccess;
 
-  e = a.mapped ? launch_attn_mapped(prm, a, stream) : dispatch_attn<false>(prm, a, stream);
+  e = !a.mapped ? dispatch_attn<false>(prm, a, stream)
+    : p.pairs   ? launch_attn_pairs(prm, a, stream)
+                : launch_attn_mapped(prm, a, stream);
   if (e != hipSuccess) return e;
   return (a.stages & 4) ? launch_merge_up(a, p, stream) : hipSuccess;
 }

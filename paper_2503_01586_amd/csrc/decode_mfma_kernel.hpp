@@ -980,5 +980,6 @@ static hipError_t dispatch_attn(const AttnParams<MAPPED>& prm, const DecodeArgs&
 }
 
 hipError_t launch_attn_mapped(const AttnMfmaParams& prm, const DecodeArgs& a, hipStream_t stream);    // decode_mfma_mapped.hip
+hipError_t launch_attn_pairs(const AttnMfmaParams& prm, const DecodeArgs& a, hipStream_t stream);     // attn_pairs.hip
 
 }  // namespace ekv

@@ -99,8 +99,9 @@ static AutoSplits balanced_splits(int64_t groups, int64_t tiles, int64_t slots) 
 // tight: the tiled fp32 kernels leave the merged latents in the place of every row's first split, the matrix-core path the
 // up-projection's partials in the place of the prepared queries, instead of a piece of their own (the same results; what was
 // there is used up, where otherwise a stage can be repeated)
+// queries: rows of B that share their sequence's cache, where the cache lies in pages or behind a tree's mask
 static int plan_decode(const elitekv_dims* d, int32_t d_ck, int64_t B, int64_t max_seq, int32_t n_splits,
-                       DecodePlan* p, bool want_fresh = false, bool block = false, bool tight = false) {
+                       DecodePlan* p, bool want_fresh = false, bool block = false, bool tight = false, int64_t queries = 1) {
   int st = check_dims(d);
   if (st) return st;
   if (B < 0 || max_seq < 0 || n_splits < 0) return ELITEKV_EINVAL;
@@ -144,13 +145,20 @@ static int plan_decode(const elitekv_dims* d, int32_t d_ck, int64_t B, int64_t m
       p->fr_ks = ks; p->fr_kc = kc; p->y_ks = yks; p->y_kc = ykc;
       p->fr_stride += d->n_heads * d->head_dim;            // x W_q is computed alongside the cache row
     }
+    const int64_t pair_groups = queries >= 2 ? Bq / queries * ((queries + 1) / 2) * p->head_groups : 0;
+    p->pairs = pair_groups > 0 && attn_pairs_pays(*d, d_ck, pair_groups, seq);
     int64_t ns = n_splits, most = n_splits;
     if (ns == 0) {
       // the narrow-latent instantiations run two work-groups per compute unit; with many batch rows
       // it pays to give every compute unit two (more splits also mean more partials to merge)
       const int64_t slots = (decode_mfma_groups_per_cu(*d) == 2 && Bq * p->head_groups >= 16) ? 2 * kComputeUnits
                                                                                              : kComputeUnits;
-      const AutoSplits a = balanced_splits(Bq * p->head_groups, (seq + 15) / 16, slots);
+      AutoSplits a = balanced_splits(Bq * p->head_groups, (seq + 15) / 16, slots);
+      if (p->pairs) {                                      // (shorter bounds may be counted as above)
+        const int64_t singles = a.most;
+        a = balanced_splits(pair_groups, (seq + 31) / 32, kComputeUnits);
+        a.most = std::max(a.most, singles);
+      }
       ns = a.count; most = a.most;
       p->least_splits = (int32_t)a.one_round;
     }
@@ -480,7 +488,7 @@ static int decode_impl(const elitekv_dims* dims, int32_t d_ck, const void* q, co
                        void* hip_stream, int32_t stages, int32_t q_per_seq = 1, bool tight = false,
                        const RowMap* map = nullptr) {
   DecodePlan p;
-  int st = plan_decode(dims, d_ck, B, max_seq_len, n_splits, &p, false, false, tight);
+  int st = plan_decode(dims, d_ck, B, max_seq_len, n_splits, &p, false, false, tight, map ? q_per_seq : 1);
   if (st) return st;
   st = decode_check(dims, p, q, q_pos, seq_len, B, batch_stride_rows, W_uk, W_uv, elite_idx, ke_plane, c_plane,
                     plane_rows, out, ws, ws_bytes);
@@ -1039,10 +1047,10 @@ size_t elitekv_paged_attn_workspace_bytes(const elitekv_dims* dims, int32_t d_ck
   if (prefill_flash_supported(*dims, d_ck, T, max_seq_len)) {
     if (!paged_prompt_fits(dims, B, T)) return 0;
     // (and room for a shorter bound, with which the queries are absorbed)
-    const size_t absorbed = B * T <= 65535 && plan_decode(dims, d_ck, B * T, kPromptRows, n_splits, &p) == ELITEKV_OK ? p.reserve : 0;
+    const size_t absorbed = B * T <= 65535 && plan_decode(dims, d_ck, B * T, kPromptRows, n_splits, &p, false, false, false, T) == ELITEKV_OK ? p.reserve : 0;
     return std::max(paged_prompt(dims, B, max_seq_len).off_flash + prefill_flash_workspace(*dims, B, max_seq_len), absorbed);
   }
-  return B * T > 65535 || plan_decode(dims, d_ck, B * T, max_seq_len, n_splits, &p) ? 0 : p.reserve;
+  return B * T > 65535 || plan_decode(dims, d_ck, B * T, max_seq_len, n_splits, &p, false, false, false, T) ? 0 : p.reserve;
 }
 
 int elitekv_paged_attn(const elitekv_dims* dims, int32_t d_ck, const void* q, const int32_t* q_pos, const int32_t* kv_len, int64_t B,
@@ -1094,7 +1102,7 @@ size_t elitekv_tree_attn_workspace_bytes(const elitekv_dims* dims, int32_t d_ck,
                                          int32_t n_splits) {
   DecodePlan p;
   if (B < 0 || T < 1 || T > ELITEKV_TREE_MAX_NODES || B * T > 65535 ||
-      plan_decode(dims, d_ck, B * T, max_seq_len, n_splits, &p))
+      plan_decode(dims, d_ck, B * T, max_seq_len, n_splits, &p, false, false, false, T))
     return 0;
   return p.reserve;
 }

@@ -43,6 +43,7 @@ struct DecodePlan {
   int32_t least_splits; // automatic counts: the fewest that elitekv_decode_attn_noalloc makes do with
   int32_t chunk;        // cached tokens per split
   int32_t mfma;         // 1: bf16 MFMA kernels, 0: kernels in fp32 arithmetic
+  int32_t pairs;        // rows that share their sequence's cache, two a work-group (attn_pairs.hip)
   int32_t tiled;        // mfma 0: 1: the tiled fp32 kernels (tiled_f32.hip), 0: the any-shape kernels
   int32_t head_groups;  // MFMA path: groups of up to 32 heads
   int32_t up_cw;        // MFMA path: latent columns per merge/up-projection work-group
@@ -177,6 +178,7 @@ constexpr int kGdStage = 32;                    // contraction rows per stage of
 int append_gemm_tile(const AppendArgs& a);      // the elitekv_gemm_tile that launch_append_gemm takes
 bool append_tiled_supported(const elitekv_dims& d, int64_t T, int d_ck);
 hipError_t launch_append_tiled(const AppendArgs& a, hipStream_t stream);
+bool attn_pairs_pays(const elitekv_dims& d, int d_ck, int64_t groups, int64_t max_seq);
 bool decode_tiled_supported(const elitekv_dims& d, int d_ck, int64_t rows, int64_t max_seq);
 hipError_t launch_decode_tiled(const DecodeArgs& a, const DecodePlan& p, hipStream_t stream);
 bool front_tiled_supported(const AppendArgs& ap, const DecodeArgs& a, const DecodePlan& p);

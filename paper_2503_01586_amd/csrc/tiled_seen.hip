@@ -6,14 +6,6 @@
 
 namespace ekv {
 
-// the largest of the four lanes i16, i16 + 16, ... in each of them, without a trip through LDS
-__device__ __forceinline__ float max_of_quads(float x) {
-  const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-  x = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
-  const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-  return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
-}
-
 // ---- split attention ----
 // The products of attn_tiled_kernel: work-group (8 waves) = (split, 16 heads, query row), per tile of 16 cached tokens every wave takes CPW
 // blocks of 16 latent columns; scores, maxima, sums and accumulators in fp32.  A tile of 16 rows lies inside one page.  What differs:

@@ -422,6 +422,78 @@ def test_widths_in_fp32_arithmetic(name, T, page, monkeypatch):
         assert np.all(got[1, T - 1:] == 0.0)
 
 
+# two queries a work-group: the widths that are compiled, four and eight elite chunks, one and more groups of 32 heads
+PAIRS = {
+    "768_r4": (shape(64, 8, 128, 4, 768, "bf16"), 0),
+    "768_r8_40_heads": (shape(64, 40, 128, 8, 768, "bf16"), 0),
+    "512_r8": (shape(64, 8, 64, 8, 512, "bf16"), 0),
+    "256_r4_33_heads": (shape(64, 33, 64, 4, 256, "bf16"), 0),
+}
+
+
+def _close_rows(name, got, ref):
+    """Queries one by one: a tile lost for one query among hundreds is not in the norm of all."""
+    norms = np.linalg.norm((got - ref).reshape(*got.shape[:2], -1), axis=2) / np.maximum(np.linalg.norm(ref.reshape(*got.shape[:2], -1), axis=2), 1e-30)
+    assert norms.max() <= 1.5e-2, (name, np.unravel_index(norms.argmax(), norms.shape), norms.max())
+
+
+@pytest.mark.parametrize("T,page", [(128, 16), (127, 64), (127, 0)])
+@pytest.mark.parametrize("name", list(PAIRS))
+def test_pairs_of_queries(name, T, page, monkeypatch):
+    """Masks that differ from query to query, nodes that see the prefix alone or nothing, an odd last query, and rows of NaN that one
+    query of a pair sees and the other does not.  One query's norm: sqrt(5) x 2^-8 / sqrt(3) x 0.72 = 3.6e-3 on average, four times that at
+    most."""
+    print("pairs", name, T, page, flush=True)
+    monkeypatch.setitem(SHAPES, name, PAIRS[name])
+    prefix, nodes = np.array([490, 0, 333]), np.array([T, T - 3, T])
+    lens = [int(p + n) for p, n in zip(prefix, nodes)]
+    k = Cache(name, lens, page, seed=T + page)
+    q = k.queries(T)
+    sees = np.stack([orc.tree_sees(_random_tree(k.rng, T), n) for n in nodes])
+    sees[2] = k.rng.random((T, T)) < 0.4
+    sees[2, 10] = sees[2, 11] = sees[2, 40] = False
+    for node in (6, 51):                                   # seen by one query alone
+        sees[2, :, node] = False
+        sees[2, node, node] = True
+        row = int(k.rows[2][prefix[2] + node])
+        k.c[row], k.ke[row] = float("nan"), float("inf")
+    pos = prefix[:, None] + np.maximum(sees.sum(axis=2) - 1, 0)
+    seen = []
+    for b, n in enumerate(lens):
+        s = np.zeros((T, n), dtype=bool)
+        s[:nodes[b], :prefix[b]] = True
+        s[:, prefix[b]:] = sees[b][:, :nodes[b]]
+        seen.append(s)
+    with np.errstate(invalid="ignore"):
+        ref = k.reference(q, pos, seen)
+    bound = -(-(12 * 256) // (3 * ((T + 1) // 2))) * 32    # tiles enough for two queries a work-group
+    for ns in (0, 1, 2, 5):
+        got = host64(k.tree(q, pos, prefix, nodes, sees, ns, max_seq=max(bound, max(lens)) if not page else None))
+        for node in (6, 51):
+            assert not np.any(np.isfinite(got[2, node])), node
+            got[2, node] = ref[2, node] = 0.0
+        _close("%s T %d page %d splits %d" % (name, T, page, ns), got, ref, k.dt)
+        _close_rows(name, got, ref)
+        assert np.all(got[1, T - 3:] == 0.0)
+
+
+@pytest.mark.parametrize("name", ["768_r4", "512_r8"])
+def test_pairs_of_queries_over_pages(name, monkeypatch):
+    """Drafted chains: every query sees one row more than the one before it, from none to all."""
+    monkeypatch.setitem(SHAPES, name, PAIRS[name])
+    T, lens = 47, [1200, 47, 700, 33]
+    k = Cache(name, lens, 32, seed=81)
+    q = k.queries(T)
+    kv = np.array([[max(n - T + t + 1, 0) for t in range(T)] for n in lens])
+    pos = np.maximum(kv - 1, 0)
+    ref = k.reference(q, pos, [np.arange(n)[None] < kv[b][:, None] for b, n in enumerate(lens)])
+    for ns in (0, 1, 7):
+        got = host64(k.paged(q, pos, kv, ns))
+        _close("%s splits %d" % (name, ns), got, ref, k.dt)
+        _close_rows(name, got, ref)
+        assert np.all(got[kv == 0] == 0.0)
+
+
 MANY = {
     "72_heads": (shape(64, 72, 128, 16, 256, "bf16"), 0),
     "head_64": (shape(64, 72, 64, 4, 128, "bf16"), 0),
