@@ -17,7 +17,8 @@
 //
 // 8 trees of 64 nodes behind 2048 to 512 tokens, 7B 12.5 %: 167 us, 460 TFLOP/s (one query a work-group: 192); a step takes 2.5 us: 0.75
 // of products, the rest the chain and a wave's own instructions, 320 vector ones a step, with no second wave to fill in.  With the rows
-// requested ahead of all products and stored behind them 200; with exp2f, which also takes care of denormals, 179.
+// requested ahead of all products and stored behind them 200; with exp2f, which also takes care of denormals, 179.  3 trees of 26 behind
+// 5001 to 2833 tokens, latents of 768 + 768: 108 us, 290 TFLOP/s (one query a work-group 193).
 #include "decode_mfma_kernel.hpp"
 
 namespace ekv {
@@ -34,7 +35,10 @@ struct PairsLayout {
   static_assert(32 * TSTR <= SLICE && BYTES <= 160 * 1024 && DC_W % 64 == 0, "");
 };
 
-template <int DC_W, int TWO_R>
+// SEP: separated latents of two halves.  A wave has a quarter of the key latents' columns and one of the value latents', which take the
+// former's place in LDS behind the score products: value latents are on their way during the scores, the next tile's key latents and elite
+// keys from there on.
+template <int DC_W, int TWO_R, bool SEP>
 __global__ __launch_bounds__(256, 1) void attn_pairs_kernel(const AttnMfmaMappedParams p) {
   using L = PairsLayout<DC_W, TWO_R>;
   constexpr int KS = DC_W / 16, ES = TWO_R / 2, CT = DC_W / 32, CB = DC_W / 64;
@@ -123,6 +127,7 @@ __global__ __launch_bounds__(256, 1) void attn_pairs_kernel(const AttnMfmaMapped
   u32x4 stage[NL];
   const int64_t crow = (int64_t)p.d_c * 2, krow = (int64_t)p.n_h * TWO_R * 2;
   const char* cbase = reinterpret_cast<const char*>(p.c_plane) + wave * DC_W * 2;
+  const int64_t v_off = SEP ? (int64_t)p.d_q * 2 : 0;       // bytes from the key latents of a row to its value latents
   const char* kbase = reinterpret_cast<const char*>(p.ke_plane);
   // 16-byte piece of the eight heads' keys that this lane loads
   const uint32_t kpiece = lane & (TWO_R - 1);
@@ -144,14 +149,14 @@ __global__ __launch_bounds__(256, 1) void attn_pairs_kernel(const AttnMfmaMapped
     for (int rg = 0; rg < 4; ++rg) rows[rg] = s.u == 0xffffffffu ? (uint32_t)((rg & 1) * 8 + (lane >> 3)) : row_of(rg * 8 + (lane >> 3));
   };
   // piece i of a step: the elite keys' first, then the column blocks, four pieces of eight rows each
-  auto fetch = [&](int i) {
+  auto fetch = [&](int i, int64_t off = 0) {
     if (i < KL) {
       constexpr int RPL = 64 / TWO_R;                       // rows of a piece
       const uint32_t r = TWO_R == 8 ? rows[i & 3] : row_of(i * RPL + lane / TWO_R);
       stage[i] = *reinterpret_cast<const u32x4*>((i * RPL < 16 ? k0 : k1) + r * (uint32_t)krow + kcol);
     } else {
       const int cb = (i - KL) >> 2, rg = (i - KL) & 3;
-      stage[i] = *reinterpret_cast<const u32x4*>((rg < 2 ? c0 : c1) + cb * 128 + (rows[rg] * (uint32_t)crow + (lane & 7) * 16));
+      stage[i] = *reinterpret_cast<const u32x4*>((rg < 2 ? c0 : c1) + off + cb * 128 + (rows[rg] * (uint32_t)crow + (lane & 7) * 16));
     }
   };
   char* slice = smem + wave * L::SLICE;
@@ -208,7 +213,7 @@ __global__ __launch_bounds__(256, 1) void attn_pairs_kernel(const AttnMfmaMapped
         if constexpr (A) da = __builtin_amdgcn_mfma_f32_32x32x16_bf16(c[ks % LOOK], fa, da, 0, 0, 0);
         if constexpr (B) db = __builtin_amdgcn_mfma_f32_32x32x16_bf16(c[ks % LOOK], fb, db, 0, 0, 0);
         if (ks + LOOK < KS + ES) c[ks % LOOK] = *reinterpret_cast<const bf16x8*>(arow + (ks + LOOK) * 32);
-        fetch(ks);                                           // (as many pieces as products)
+        if constexpr (!SEP) fetch(ks);                       // (as many pieces as products)
         __builtin_amdgcn_sched_barrier(0);
       }
     }
@@ -224,6 +229,12 @@ __global__ __launch_bounds__(256, 1) void attn_pairs_kernel(const AttnMfmaMapped
     };
     if constexpr (A) part(da, 0);
     if constexpr (B) part(db, 1);
+    if constexpr (SEP) {
+#pragma unroll
+      for (int i = KL; i < NL; ++i) settle(i);               // the value latents (the key latents have been read)
+#pragma unroll
+      for (int i = 0; i < NL; ++i) fetch(i);
+    }
     __syncthreads();
 
     // ---- the rows of this wave: sum of the parts, maximum, probabilities
@@ -322,6 +333,10 @@ __global__ __launch_bounds__(256, 1) void attn_pairs_kernel(const AttnMfmaMapped
       }
       __builtin_amdgcn_sched_barrier(0);
     }
+    if constexpr (SEP) {
+#pragma unroll
+      for (int i = KL; i < NL; ++i) fetch(i, v_off);
+    }
     pin();
   };
 
@@ -336,6 +351,10 @@ __global__ __launch_bounds__(256, 1) void attn_pairs_kernel(const AttnMfmaMapped
     for (int i = 0; i < NL; ++i) fetch(i);
 #pragma unroll
     for (int i = 0; i < NL; ++i) settle(i);
+    if constexpr (SEP) {
+#pragma unroll
+      for (int i = KL; i < NL; ++i) fetch(i, v_off);
+    }
     while (cur.j >= 0) {
       const Step ahead = next(with_a, with_b);
       if (ahead.j >= 0) aim(ahead);
@@ -383,30 +402,36 @@ __global__ __launch_bounds__(256, 1) void attn_pairs_kernel(const AttnMfmaMapped
   if (two) store(ub, ib);
 }
 
-template <int DC_W, int TWO_R>
+template <int DC_W, int TWO_R, bool SEP>
 static hipError_t launch_pairs(AttnMfmaMappedParams& prm, hipStream_t stream) {
   using L = PairsLayout<DC_W, TWO_R>;
   static LdsLimit limit;
-  const hipError_t e = raise_lds_limit(limit, reinterpret_cast<const void*>(&attn_pairs_kernel<DC_W, TWO_R>), L::BYTES);
+  const hipError_t e = raise_lds_limit(limit, reinterpret_cast<const void*>(&attn_pairs_kernel<DC_W, TWO_R, SEP>), L::BYTES);
   if (e != hipSuccess) return e;
   const int readers = (prm.q_per_seq + 1) / 2 * prm.head_groups, all = prm.n_splits * (prm.batch / prm.q_per_seq) * readers;
   prm.reader_run = reader_run(readers, all);
   prm.reader_turns = reader_turns(all, prm.reader_run);
   const int grid = 8 * (prm.reader_turns * prm.reader_run + (all - prm.reader_turns * 8 * prm.reader_run + 7) / 8);
-  attn_pairs_kernel<DC_W, TWO_R><<<grid, 256, L::BYTES, stream>>>(prm);
+  attn_pairs_kernel<DC_W, TWO_R, SEP><<<grid, 256, L::BYTES, stream>>>(prm);
   return hipGetLastError();
 }
 
-constexpr int64_t kPairsTiles = 12;
-
-// groups: (pair of queries, group of 32 heads) of all sequences.  From a dozen tiles a compute unit on: a work-group's start, two queries'
-// with one wave per SIMD, takes 7 us more than one query's.  Trees of T nodes, B x T x rows (tiles a compute unit), us, one query a
-// work-group / two: 7B 12.5 % (768 columns, four chunks) 4 x 5 x 4096 (6) 50.4 / 55.8, 16 x 4 x 2000 (8) 62.4 / 63.4, 4 x 26 x 2000 (13)
-// 82.2 / 83.7, 8 x 64 x 2048 (64) 241.3 / 208.3; 768 columns, eight chunks 57.8 / 58.0, 75.3 / 66.6, 118 / 86.7, 394 / 225; 512 columns
-// 45.0 / 48.4, 55.0 / 55.1, 70.8 / 69.2, 228 / 186; 256 columns 37.2 / 39.4, 46.2 / 44.7, 57.5 / 54.3, 177 / 138.
+// groups: (pair of queries, group of 32 heads) of all sequences.  A work-group's start, two queries' with one wave per SIMD, takes 7 us more
+// than one query's, so there have to be enough tiles a compute unit: four where the kernel of one query has a compute unit to itself, eight
+// where two of its work-groups share one.  Trees or drafted chains, queries x rows (tiles a compute unit), us, one query a work-group / two:
+//                      1 x 8 x 6000 (2.9)  2 x 16 x 2000 (3.9)  4 x 5 x 4096 (6)  16 x 4 x 2000 (7.9)  4 x 26 x 2000 (13)  8 x 64 x 2048 (64)
+//   768 + 768, r = 8     50.5 / 54.3         60.2 / 58.4          68.2 / 64.6       94.6 / 81.0          142.8 / 98.7        496 / 275
+//   512 + 512, r = 8     47.2 / 45.9         54.1 / 47.5          61.7 / 52.2       82.3 / 60.9          128.3 / 75.7        461 / 215
+//   768, r = 8           46.0 / 52.1         52.5 / 55.0          58.1 / 58.8       75.4 / 67.8          118.0 / 87.5        394 / 225
+//   256 + 256, r = 4     39.7 / 39.2         38.0 / 37.7          40.5 / 40.2       51.5 / 46.5          63.6 / 55.4         203 / 144
+//   768, r = 4           43.7 / 50.2         47.5 / 53.5          49.8 / 55.8       64.6 / 65.4          82.2 / 83.0         241 / 209
+//   512, r = 8           40.4 / 44.4         42.1 / 45.2          44.9 / 48.6       56.5 / 55.9          70.8 / 69.2         228 / 187
+//   256, r = 4           36.5 / 38.5         35.6 / 37.1          37.3 / 39.1       47.1 / 45.6          57.5 / 54.3         177 / 138
 bool attn_pairs_pays(const elitekv_dims& d, int d_ck, int64_t groups, int64_t max_seq) {
-  return decode_mfma_supported(d, d_ck) && d_ck == 0 && (d.r == 4 || d.r == 8) && (d.d_c == 768 || d.d_c == 512 || d.d_c == 256) &&
-         groups * ((max_seq + 31) / 32) >= kPairsTiles * 256;
+  const int half = d_ck ? d.d_c - d_ck : d.d_c;
+  return decode_mfma_supported(d, d_ck) && (d_ck == 0 || d_ck == half) && (d.r == 4 || d.r == 8) &&
+         (half == 768 || half == 512 || half == 256) &&
+         groups * ((max_seq + 31) / 32) >= (decode_mfma_groups_per_cu(d) == 1 ? 4 : 8) * 256;
 }
 
 hipError_t launch_attn_pairs(const AttnMfmaParams& prm, const DecodeArgs& a, hipStream_t stream) {
@@ -415,7 +440,9 @@ hipError_t launch_attn_pairs(const AttnMfmaParams& prm, const DecodeArgs& a, hip
   p.map = a.map;
   const elitekv_dims& d = a.dims;
 #define EKV_PAIRS(W) \
-  if (d.d_c == 4 * W) return d.r == 4 ? launch_pairs<W, 8>(p, stream) : launch_pairs<W, 16>(p, stream);
+  if (prm.d_u == 4 * W)                                                                                                       \
+    return a.d_ck ? (d.r == 4 ? launch_pairs<W, 8, true>(p, stream) : launch_pairs<W, 16, true>(p, stream))                    \
+                  : d.r == 4 ? launch_pairs<W, 8, false>(p, stream) : launch_pairs<W, 16, false>(p, stream);
   EKV_PAIRS(64) EKV_PAIRS(128) EKV_PAIRS(192)
 #undef EKV_PAIRS
   return hipErrorInvalidValue;

@@ -428,6 +428,9 @@ PAIRS = {
     "768_r8_40_heads": (shape(64, 40, 128, 8, 768, "bf16"), 0),
     "512_r8": (shape(64, 8, 64, 8, 512, "bf16"), 0),
     "256_r4_33_heads": (shape(64, 33, 64, 4, 256, "bf16"), 0),
+    "slrd_768": (shape(64, 8, 128, 8, 1536, "bf16"), 768),
+    "slrd_512_r4_40_heads": (shape(64, 40, 128, 4, 1024, "bf16"), 512),
+    "slrd_256": (shape(64, 5, 64, 8, 512, "bf16"), 256),
 }
 
 
@@ -477,7 +480,7 @@ def test_pairs_of_queries(name, T, page, monkeypatch):
         assert np.all(got[1, T - 3:] == 0.0)
 
 
-@pytest.mark.parametrize("name", ["768_r4", "512_r8"])
+@pytest.mark.parametrize("name", ["768_r4", "512_r8", "slrd_768", "slrd_256"])
 def test_pairs_of_queries_over_pages(name, monkeypatch):
     """Drafted chains: every query sees one row more than the one before it, from none to all."""
     monkeypatch.setitem(SHAPES, name, PAIRS[name])
