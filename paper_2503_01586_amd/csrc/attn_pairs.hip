@@ -18,7 +18,7 @@
 // 8 trees of 64 nodes behind 2048 to 512 tokens, 7B 12.5 %: 167 us, 460 TFLOP/s (one query a work-group: 192); a step takes 2.5 us: 0.75
 // of products, the rest the chain and a wave's own instructions, 320 vector ones a step, with no second wave to fill in.  With the rows
 // requested ahead of all products and stored behind them 200; with exp2f, which also takes care of denormals, 179.  3 trees of 26 behind
-// 5001 to 2833 tokens, latents of 768 + 768: 108 us, 290 TFLOP/s (one query a work-group 193).
+// 5001 to 2833 tokens, latents of 768 + 768: 104 us, 300 TFLOP/s (one query a work-group 193).
 #include "decode_mfma_kernel.hpp"
 
 namespace ekv {
@@ -231,9 +231,10 @@ __global__ __launch_bounds__(256, 1) void attn_pairs_kernel(const AttnMfmaMapped
     if constexpr (B) part(db, 1);
     if constexpr (SEP) {
 #pragma unroll
-      for (int i = KL; i < NL; ++i) settle(i);               // the value latents (the key latents have been read)
-#pragma unroll
-      for (int i = 0; i < NL; ++i) fetch(i);
+      for (int i = 0; i < NL; ++i) {
+        if (i >= KL) settle(i);                              // the value latents (the key latents have been read)
+        fetch(i);
+      }
     }
     __syncthreads();
 
@@ -420,7 +421,7 @@ static hipError_t launch_pairs(AttnMfmaMappedParams& prm, hipStream_t stream) {
 // than one query's, so there have to be enough tiles a compute unit: four where the kernel of one query has a compute unit to itself, eight
 // where two of its work-groups share one.  Trees or drafted chains, queries x rows (tiles a compute unit), us, one query a work-group / two:
 //                      1 x 8 x 6000 (2.9)  2 x 16 x 2000 (3.9)  4 x 5 x 4096 (6)  16 x 4 x 2000 (7.9)  4 x 26 x 2000 (13)  8 x 64 x 2048 (64)
-//   768 + 768, r = 8     50.5 / 54.3         60.2 / 58.4          68.2 / 64.6       94.6 / 81.0          142.8 / 98.7        496 / 275
+//   768 + 768, r = 8     50.5 / 54.3         60.2 / 58.4          68.2 / 63.4       94.6 / 79.3          142.8 / 94.8        496 / 270
 //   512 + 512, r = 8     47.2 / 45.9         54.1 / 47.5          61.7 / 52.2       82.3 / 60.9          128.3 / 75.7        461 / 215
 //   768, r = 8           46.0 / 52.1         52.5 / 55.0          58.1 / 58.8       75.4 / 67.8          118.0 / 87.5        394 / 225
 //   256 + 256, r = 4     39.7 / 39.2         38.0 / 37.7          40.5 / 40.2       51.5 / 46.5          63.6 / 55.4         203 / 144
