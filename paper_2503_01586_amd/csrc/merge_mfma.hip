@@ -271,9 +271,9 @@ __global__ __launch_bounds__(256) void merge_up_mfma_kernel(
 // columns one after the other, so that the up-projection's sum stays in the accumulators instead of a partial per stage in memory (512
 // rows of 32 heads and 768 columns: 50 MB written, and read again by out_reduce).  The arithmetic of merge_up_mfma_kernel: merged,
 // normalised latents in fp32, as bf16 high part + remainder.  The two parts lie in LDS, [64 rows][128 columns] each, so that sixteen lanes
-// read 256 bytes of one row of the accumulators (a lane per row, as the operand of the product would have it, touches 32 pages of memory
-// with every load: 38 us for 512 rows); a stage's loads are requested while the stage before is multiplied.  512 rows of 32 heads, 768
-// columns, one split: 31 us (merge_up_mfma_kernel and out_reduce_kernel 52), for 25 MB of accumulators and W_uv once per 64 rows.
+// read 256 bytes of one row of the accumulators; a stage's loads are requested while the stage before is multiplied.  512 rows of 32 heads,
+// 768 columns, one split: 16.7 us (merge_up_mfma_kernel and out_reduce_kernel 52), for 25 MB of accumulators and W_uv once per 64 rows.
+// (Stages as arrays of vector types: as arrays of structs they go through scratch memory and the loads one by one, 31 us.)
 constexpr int kMrThreads = 256, kMrRows = 64, kMrSplits = 4;
 constexpr int kMrURow = kMmCols * 2 + 16;                   // bytes of a row of a part in LDS (padded)
 
@@ -291,7 +291,7 @@ __global__ __launch_bounds__(kMrThreads) void merge_rows_kernel(const float* __r
 
   constexpr int CPR = DH / 8, WPASS = kMmCols * CPR / kMrThreads, UPASS = kMrRows * 16 / kMrThreads;
   const int cl = tid & 15, r0 = tid >> 4;                  // this thread's 16 bytes of rows r0, r0 + 16, ...
-  uint4 wld[WPASS], uld[UPASS][NP];
+  ekv_u32x4 wld[WPASS], uld[UPASS][NP];
   const bf16_t* ub[UPASS];
   float scale[UPASS][NP];
 #pragma unroll
@@ -320,12 +320,12 @@ __global__ __launch_bounds__(kMrThreads) void merge_rows_kernel(const float* __r
 #pragma unroll
     for (int i = 0; i < WPASS; ++i) {
       const int e = i * kMrThreads + tid, k = e / CPR, c = e % CPR;
-      wld[i] = *reinterpret_cast<const uint4*>(W_uv + ((int64_t)min(k0 + k, d_u - 1) * n_h + head) * DH + c * 8);
+      wld[i] = *reinterpret_cast<const ekv_u32x4*>(W_uv + ((int64_t)min(k0 + k, d_u - 1) * n_h + head) * DH + c * 8);
     }
 #pragma unroll
     for (int j = 0; j < UPASS; ++j)
 #pragma unroll
-      for (int s = 0; s < NP; ++s) uld[j][s] = *reinterpret_cast<const uint4*>(ub[j] + (int64_t)s * nhp * d_u + min(k0 + cl * 8, d_u - 8));
+      for (int s = 0; s < NP; ++s) uld[j][s] = *reinterpret_cast<const ekv_u32x4*>(ub[j] + (int64_t)s * nhp * d_u + min(k0 + cl * 8, d_u - 8));
   };
   load(0);
   mm_f32x16 acc[NT];
@@ -342,7 +342,7 @@ __global__ __launch_bounds__(kMrThreads) void merge_rows_kernel(const float* __r
       if (k0 + cl * 8 < d_u) {                             // (a last stage of 64 columns: zeros against what repeats the last one)
 #pragma unroll
         for (int s = 0; s < NP; ++s) {
-          const uint32_t uu[4] = {uld[j][s].x, uld[j][s].y, uld[j][s].z, uld[j][s].w};
+          const ekv_u32x4 uu = uld[j][s];
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             f[2 * i] = fmaf(scale[j][s], __uint_as_float(uu[i] << 16), f[2 * i]);
@@ -363,7 +363,7 @@ __global__ __launch_bounds__(kMrThreads) void merge_rows_kernel(const float* __r
 #pragma unroll
     for (int i = 0; i < WPASS; ++i) {
       const int e = i * kMrThreads + tid, k = e / CPR, c = e % CPR;
-      *reinterpret_cast<uint4*>(wst + k * WROW + c * 16) = wld[i];
+      *reinterpret_cast<ekv_u32x4*>(wst + k * WROW + c * 16) = wld[i];
     }
     __syncthreads();
     if (k0 + kMmCols < d_u) load(k0 + kMmCols);
@@ -420,6 +420,9 @@ static hipError_t launch_merge_mfma_dh(const DecodeArgs& a, const DecodePlan& p,
   return hipGetLastError();
 }
 
+// From a work-group a compute unit on, and up to four splits (registers of a stage).  Below, a work-group's stages one after the other cost
+// more than a partial per stage: trees of n nodes, us, partials / this, for up to eight splits: 7B 12.5 % 16 x 4 over 2000 64.0 / 80.7,
+// 1 x 64 over 300 43.4 / 57.5, 3 x 26 over 5001 107 / 114; 768 + 768 columns 127 / 135.
 bool merge_rows_pays(const DecodeArgs& a, const DecodePlan& p) {
   return a.mapped && p.merge_batch && p.n_part <= kMrSplits && (a.B + kMrRows - 1) / kMrRows * a.dims.n_heads >= 256;
 }
