@@ -497,6 +497,45 @@ def test_pairs_of_queries_over_pages(name, monkeypatch):
         assert np.all(got[kv == 0] == 0.0)
 
 
+def test_pairs_of_queries_replay_from_a_graph(monkeypatch):
+    """A captured call replayed between the program's own work, with other trees and lengths in its arrays: every replay is the eager call."""
+    name, T = "768_r4", 64
+    monkeypatch.setitem(SHAPES, name, PAIRS[name])
+    lens = [900, 300, 64, 1100]
+    k = Cache(name, lens, 16, seed=91)
+    q = k.queries(T)
+    bound = 1600                                           # 128 pairs x 50 tiles: two queries a work-group
+    prefix, nodes = i32([0] * 4), i32([0] * 4)
+    pos, mask = i32(np.zeros((4, T))), i32(np.zeros((4, T, 2)))
+    out = k.blank(q)
+    ws = torch.full((ekv.elitekv_tree_attn_workspace_bytes(k.dims, 4, T, bound),), 0xFF, dtype=torch.uint8, device=DEV)
+    args = (k.dims, q, pos, prefix, nodes, mask, bound, 0, k.W_uk, k.W_uv, i32(k.idx), k.ke, k.c, out, ws)
+    table = i32(k.table)
+    call = lambda: ekv.elitekv_tree_attn(*args, block_table=table, page_rows=16)
+    call()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    for seed in range(3):
+        rng = np.random.default_rng(seed)
+        n = rng.integers(1, T + 1, 4)
+        sees = np.stack([orc.tree_sees(_random_tree(rng, T), int(m)) for m in n])
+        nodes.copy_(i32(n))
+        prefix.copy_(i32(np.array(lens) - n))
+        pos.copy_(i32((np.array(lens) - n)[:, None] + np.maximum(sees.sum(axis=2) - 1, 0)))
+        mask.copy_(torch.from_numpy(orc.mask_words(sees).view(np.int32)).to(DEV))
+        out.fill_(float("nan"))
+        graph.replay()
+        torch.cuda.synchronize()
+        replayed = out.clone()
+        out.fill_(float("nan"))
+        call()
+        torch.cuda.synchronize()
+        assert torch.equal(replayed, out) and torch.all(torch.isfinite(out.float()))
+        assert torch.all(out[0, int(n[0]):] == 0) and torch.any(out[0, 0] != 0)
+
+
 MANY = {
     "72_heads": (shape(64, 72, 128, 16, 256, "bf16"), 0),
     "head_64": (shape(64, 72, 64, 4, 128, "bf16"), 0),

@@ -144,3 +144,18 @@ def test_tree_plan_and_commit_refusals():
     for k in ("ke", "c"):
         assert commit(d, **{k: FAKE + 4}) == ekv.EALIGN, k
     assert commit(_dims(r=0), ke=None, B=0) == ekv.OK
+
+
+@pytest.mark.parametrize("B,T", [(1, 2), (1, 64), (3, 26), (8, 5), (8, 64), (64, 3), (200, 128)])
+@pytest.mark.parametrize("shape,d_ck", [(dict(r=4, d_c=768), 0), (dict(r=8, d_c=768), 0), (dict(r=8, d_c=512, n_heads=40), 0), (dict(r=4, d_c=256), 0),
+                                        (dict(r=8, d_c=1536), 768), (dict(r=4, d_c=512), 256), (dict(r=8, d_c=1536), 0),
+                                        (dict(r=8, d_c=1536, dtype="fp32"), 0)])
+def test_a_workspace_of_a_longer_bound_serves_every_shorter_one(shape, d_ck, B, T):
+    """Also across the length from which two queries share a work-group, which are split by another count."""
+    d = _dims(**dict(dict(n_heads=32, head_dim=128, dtype="bf16"), **shape))
+    bounds = list(range(0, 200, 7)) + list(range(200, 9000, 37)) + [20000, 131072]
+    sizes = [ekv.elitekv_tree_attn_workspace_bytes(d, B, T, s, d_ck=d_ck) for s in bounds]
+    assert sizes == sorted(sizes) and sizes[0] > 0
+    if T < 48:
+        paged = [ekv.elitekv_paged_attn_workspace_bytes(d, B, T, s, d_ck=d_ck) for s in bounds]
+        assert paged == sizes
