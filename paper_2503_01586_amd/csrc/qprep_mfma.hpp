@@ -26,7 +26,12 @@ constexpr int kQmRows = 64;     // batch rows staged in LDS per pass
 // LDS bytes of the body: the compacted non-elite query of kQmRows batch rows + the chunk list
 inline size_t qprep_mfma_lds(int head_dim, int r) { return (size_t)kQmRows * (head_dim - 2 * r + 8) * 2 + 64 * sizeof(int); }
 
-// bx = block of 128 latent columns, by = head; qms = qprep_mfma_lds(...) bytes of 16-byte aligned LDS;
+// MANY: rows of 256 bytes would all lie in the same banks (nd = 120: 86 % of the LDS cycles were
+// conflicts, 24 us for 512 rows instead of 19)
+__host__ __device__ inline int qprep_many_row(int nd) { return nd + 8 + ((nd + 8) % 128 == 0 ? 8 : 0); }
+inline size_t qprep_many_lds(int head_dim, int r) { return (size_t)kQmRows * qprep_many_row(head_dim - 2 * r) * 2 + 64 * sizeof(int); }
+
+// bx = block of 128 latent columns, by = head; qms = qprep_mfma_lds(...) (MANY: qprep_many_lds(...)) bytes of 16-byte aligned LDS;
 // KS = contraction steps of 16 non-elite dims (the tail is zero-filled).  P.sincos (optional) is written by the
 // work-groups that rotate the elite query.  Rows b_lo .. b_hi - 1.
 // MANY: a launch of many rows; the rows of a pass are requested all at once (one after the other, a pass waits for memory sixteen times).
@@ -41,7 +46,7 @@ __device__ __forceinline__ void qprep_mfma_body(const QprepRowsParams& P, const 
   bf16_t* __restrict__ qt = P.qt;
   const int B = b_hi, n_h = P.n_h, d_h = P.d_h, r = P.r, d_c = P.d_c;
   const float scale_log2e = P.scale_log2e;
-  const int nd = d_h - 2 * r, half = d_h / 2, ndp = nd + 8;
+  const int nd = d_h - 2 * r, half = d_h / 2, ndp = MANY ? qprep_many_row(nd) : nd + 8;
   uint16_t* qne = reinterpret_cast<uint16_t*>(qms);                       // [kQmRows][ndp] bf16 bits
   int* ne = reinterpret_cast<int*>(qms + (size_t)kQmRows * ndp * 2);      // [64] non-elite chunks, ascending
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
