@@ -420,11 +420,13 @@ static hipError_t launch_merge_mfma_dh(const DecodeArgs& a, const DecodePlan& p,
   return hipGetLastError();
 }
 
-// From a work-group a compute unit on, and up to four splits (registers of a stage).  Below, a work-group's stages one after the other cost
-// more than a partial per stage: trees of n nodes, us, partials / this, for up to eight splits: 7B 12.5 % 16 x 4 over 2000 64.0 / 80.7,
-// 1 x 64 over 300 43.4 / 57.5, 3 x 26 over 5001 107 / 114; 768 + 768 columns 127 / 135.
+// From a work-group every fourth compute unit on, and up to four splits (registers of a stage).  Below, and with more splits, a work-group's
+// stages one after the other cost more than a partial per stage.  Trees of n nodes, us, partials / this (work-groups): 7B 25 % 2 x 64 over
+// 600 84.5 / 82.5 (64), 3 x 64 123.5 / 109.5 (96), 6 x 60 over 577 222.8 / 172.4 (192); 7B 12.5 % 56.5 / 57.5, 75.9 / 66.2, 118.8 / 92.6;
+// 13B 25 % 159.8 / 147.0 (80), 272.4 / 228.9 (120), 445 / 371 (240).  32 work-groups, up to eight splits: 7B 12.5 % 16 x 4 over 2000 64.0 /
+// 80.7, 1 x 64 over 300 43.4 / 57.5; 64 with six splits, 768 + 768 columns, 3 x 26 over 5001 127 / 135.
 bool merge_rows_pays(const DecodeArgs& a, const DecodePlan& p) {
-  return a.mapped && p.merge_batch && p.n_part <= kMrSplits && (a.B + kMrRows - 1) / kMrRows * a.dims.n_heads >= 256;
+  return a.mapped && p.merge_batch && p.n_part <= kMrSplits && (a.B + kMrRows - 1) / kMrRows * a.dims.n_heads >= 64;
 }
 
 template <int DH, int NP>
